@@ -233,6 +233,68 @@ int lte_attn_decode(const lte_shape* s, const lte_conv* c, void* cache,
                     void* stream);
 
 /*
+ * Decode under eviction by accumulated attention (the heuristic that the paper's ablation compares with; the prompt's half is
+ * lte_attn_colsum + lte_select_rule(LTE_RULE_ACCUM_ATTN)): a cache whose score per row is the attention a the row has received.
+ *
+ * lte_cache_init_accum: lte_cache_init with a [B,H,T] fp32 in the place of the logits; every token of the prompt has one, and no
+ * scorer is involved.  Same cache, same size (lte_cache_bytes).
+ *
+ * lte_attn_decode_accum: one step for every (b,h), token n = tokens seen so far:
+ *   1. the token leaving the window, p = n-W (if >= 0 and R > 0), goes into the pool: appended if the pool holds fewer than R entries;
+ *      otherwise it replaces the entry of the lowest a (the youngest among equals, never a position < sink) iff a_p is strictly
+ *      greater (or stays out; a token p < sink finds no place in a pool that is full).  The step decides by the a of the steps before it;
+ *   2. o1, lse1 = attention of q1 over the ring's rows of positions > n-W, the pool after 1 and the incoming token;
+ *   3. a_j <- decay a_j + sum over the group's query heads of the weights w_gj = exp(scale q_g.k_j - lse_g), for every row attended in 2;
+ *      the incoming token starts with its own weights.  decay = 1 adds up all queries so far, 0 keeps the last query's weights alone;
+ *   4. k1, v1 and the incoming token's a take ring slot n mod W; the row of p and its a (with this step's weights) the pool entry.
+ * After a prompt's a of lte_attn_colsum, decay = 1 continues its sums.  s->tau is ignored (every token is a candidate), s->T too.
+ *   a        in   [B,H,T] fp32 (idx, cnt as written by lte_select_rule)
+ *   decay    0 .. 1
+ *   cache    in/out;   q1, k1, v1, o1, lse1 as for lte_attn_decode
+ * Deterministic.  A cache in this state does not go through the calls that read logits (lte_attn_decode, lte_attn_prefill_chunk,
+ * lte_cache_score): they would take a for logits.
+ * Errors: INVALID_ARG (decay outside 0 .. 1), UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
+ */
+int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const float* a, const int32_t* idx,
+                         const int32_t* cnt, void* cache, void* stream);
+int lte_attn_decode_accum(const lte_shape* s, float decay, void* cache, const void* q1, const void* k1, const void* v1,
+                          void* o1, float* lse1, void* stream);
+
+/*
+ * The decode cache in 4 bits: a head's rows take 1.25 d bytes in the place of 4 d (bf16).  A row is cut into groups of 32 channels:
+ *   zero = bf16(min), step = bf16((max - min) / 15), code = clamp(rint((x - zero) / step), 0, 15) (fp32 arithmetic; 0 where step is 0),
+ * and a channel reads back as zero + code step.  A group that holds a NaN or an infinity, or whose step or zero is not finite in bf16,
+ * reads back as NaN.  Scores (logits, or accumulated attention), positions and counters are those of the ordinary cache.
+ *
+ * Layout: a 256-byte header, then one block per (b,h), padded to a multiple of 256 bytes; every part starts on a multiple of 16:
+ *   key codes [W+R][d/2] bytes     value codes [W+R][d/2]        rows as in the ordinary cache, never swizzled
+ *   key parameters [W+R][d/32] {step, zero} bf16                 value parameters likewise
+ *   scores [W+R] fp32              pool positions [R] int32      {n, cnt, 0, 0} int32
+ * Order of a row's codes, lowest nibble first: the keys' 4-byte word j holds channels 8t .. 8t+7 of group j mod (d/32), t = j / (d/32);
+ * the values' 2-byte unit u channels 4g .. 4g+3 of group u mod (d/32), g = u / (d/32).
+ *
+ * lte_cache4_pack rounds an ordinary cache (of s->dtype) into 4 bits, lte_cache4_unpack writes the values back into an ordinary cache
+ * (bf16: rounded to it), e.g. for lte_attn_prefill_chunk when a conversation goes on; neither changes its input.  Both caches are whole
+ * and must not overlap.  lte_cache4_bytes is 0 for a shape that the calls refuse.  s->T is ignored.
+ * Errors: INVALID_ARG, UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
+ */
+size_t lte_cache4_bytes(const lte_shape* s);
+int lte_cache4_pack(const lte_shape* s, const void* cache, void* cache4, void* stream);
+int lte_cache4_unpack(const lte_shape* s, const void* cache4, void* cache, void* stream);
+
+/*
+ * One decode step over a cache in 4 bits: lte_attn_decode (the learned rule; the single-layer scorer, which reads the ring's rows as the
+ * cache holds them) and lte_attn_decode_accum.  q1, k1, v1, o1 are of s->dtype; the incoming token is attended and scored as given,
+ * and rounded to 4 bits when it takes its ring slot; a row that moves into the pool keeps its codes.
+ * Errors: as lte_attn_decode_accum; the learned rule: INVALID_ARG for what lte_attn_decode refuses in the scorer, UNSUPPORTED for the
+ * three-layer stack.
+ */
+int lte_attn_decode4(const lte_shape* s, const lte_conv* c, void* cache4, const void* q1, const void* k1, const void* v1,
+                     void* o1, float* lse1, void* stream);
+int lte_attn_decode4_accum(const lte_shape* s, float decay, void* cache4, const void* q1, const void* k1, const void* v1,
+                           void* o1, float* lse1, void* stream);
+
+/*
  * Lazy scoring of the ring (Section 3.1.3, "Cached prefilling and decoding": scores are computed in batches, each
  * before its tokens leave the window), for the three-layer stack (lte_conv.n_layers = 3), which lte_attn_decode does
  * not evaluate inside the step: every token in the ring whose receptive field (6 tokens to either side) lies inside

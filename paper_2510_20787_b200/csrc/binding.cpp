@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -247,6 +248,88 @@ LTE_FN(attn_prefill_chunk, 11)
     return pack({o.result(), lse.result()});
 }
 
+// The calls on caches that evict by accumulated attention or hold 4 bits act on the cache's device and check what they are given against
+// the shape: a cache that is too short, or a tensor of another size, type or device, would be read past its end.
+const at::Tensor& on(PyObject* o, const at::Tensor& cache, int64_t numel, at::ScalarType type, const char* text)
+{
+    const at::Tensor& t = tensor(o);
+    ptr(o, type);
+    if (t.numel() != numel || t.device() != cache.device()) fail(PyExc_ValueError, text);
+    return t;
+}
+const at::Tensor& cache_tensor(PyObject* o, size_t need)
+{
+    const at::Tensor& t = tensor(o);
+    ptr(o, at::kByte);
+    if ((size_t)t.numel() < need) fail(PyExc_ValueError, "the cache is shorter than this shape's");
+    return t;
+}
+at::ScalarType element(const lte_shape* s) { return s->dtype == LTE_BF16 ? at::kBFloat16 : at::kFloat; }
+
+// s, k, v, a, idx, cnt, cache
+LTE_FN(cache_init_accum, 7)
+{
+    const lte_shape* s = c_struct<lte_shape>(a[0]);
+    const at::Tensor& cache = cache_tensor(a[6], lte_cache_bytes(s));
+    const c10::cuda::CUDAGuard guard(cache.device());
+    const void *k = nullptr, *v = nullptr;
+    const float* score = nullptr;
+    const int32_t *idx = nullptr, *cnt = nullptr;
+    if (s->T > 0) {
+        const int64_t heads = (int64_t)s->B * s->H;
+        k = on(a[1], cache, heads * s->T * s->d, element(s), "k: another size or device than the cache's").data_ptr();
+        v = on(a[2], cache, heads * s->T * s->d, element(s), "v: another size or device than the cache's").data_ptr();
+        score = (const float*)on(a[3], cache, heads * s->T, at::kFloat, "a: another size or device than the cache's").data_ptr();
+        idx = (const int32_t*)on(a[4], cache, heads * s->R, at::kInt, "idx: another size or device than the cache's").data_ptr();
+        cnt = (const int32_t*)on(a[5], cache, heads, at::kInt, "cnt: another size or device than the cache's").data_ptr();
+    }
+    void* p = cache.data_ptr();
+    call("lte_cache_init_accum", [&](void* st) { return lte_cache_init_accum(s, k, v, score, idx, cnt, p, st); });
+    return Py_NewRef(a[6]);
+}
+
+// s, c or None (accumulated attention), decay, cache, q1, k1, v1, o1, lse1, in 4 bits
+LTE_FN(attn_decode_rows, 10)
+{
+    const lte_shape* s = c_struct<lte_shape>(a[0]);
+    const lte_conv* c = a[1] == Py_None ? nullptr : c_struct<lte_conv>(a[1]);
+    const float decay = (float)PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred()) throw PyFailure();
+    const bool four = a[9] == Py_True;
+    const at::Tensor& cache = cache_tensor(a[3], four ? lte_cache4_bytes(s) : lte_cache_bytes(s));
+    const c10::cuda::CUDAGuard guard(cache.device());
+    const int64_t heads = (int64_t)s->B * s->H, hq = heads_q(s);
+    const at::Tensor& q = on(a[4], cache, s->B * hq * s->d, element(s), "q1: another size or device than the cache's");
+    const void* k1 = on(a[5], cache, heads * s->d, element(s), "k1: another size or device than the cache's").data_ptr();
+    const void* v1 = on(a[6], cache, heads * s->d, element(s), "v1: another size or device than the cache's").data_ptr();
+    if (a[7] != Py_None) on(a[7], cache, q.numel(), element(s), "o1: another size or device than the cache's");
+    if (a[8] != Py_None) on(a[8], cache, s->B * hq, at::kFloat, "lse1: another size or device than the cache's");
+    Out o(a[7], q.sizes(), q.scalar_type(), q), lse(a[8], {s->B, hq}, at::kFloat, q);
+    const void* qp = q.data_ptr();
+    void *cp = cache.data_ptr(), *op = o.as<void>();
+    float* lp = lse.as<float>();
+    if (!four) call("lte_attn_decode_accum", [&](void* st) { return lte_attn_decode_accum(s, decay, cp, qp, k1, v1, op, lp, st); });
+    else if (c) call("lte_attn_decode4", [&](void* st) { return lte_attn_decode4(s, c, cp, qp, k1, v1, op, lp, st); });
+    else call("lte_attn_decode4_accum", [&](void* st) { return lte_attn_decode4_accum(s, decay, cp, qp, k1, v1, op, lp, st); });
+    return pack({o.result(), lse.result()});
+}
+
+// s, from, to, into 4 bits
+LTE_FN(cache4_convert, 4)
+{
+    const lte_shape* s = c_struct<lte_shape>(a[0]);
+    const bool into = a[3] == Py_True;
+    const at::Tensor& from = cache_tensor(a[1], into ? lte_cache_bytes(s) : lte_cache4_bytes(s));
+    const at::Tensor& to = cache_tensor(a[2], into ? lte_cache4_bytes(s) : lte_cache_bytes(s));
+    if (from.device() != to.device()) fail(PyExc_ValueError, "the two caches are on different devices");
+    const c10::cuda::CUDAGuard guard(from.device());
+    const void* f = from.data_ptr();
+    void* t = to.data_ptr();
+    if (into) call("lte_cache4_pack", [&](void* st) { return lte_cache4_pack(s, f, t, st); });
+    else call("lte_cache4_unpack", [&](void* st) { return lte_cache4_unpack(s, f, t, st); });
+    return Py_NewRef(a[2]);
+}
+
 // s, z, lam, ws
 LTE_FN(sparsity_stats, 4)
 {
@@ -321,7 +404,7 @@ PyObject* set_error(PyObject*, PyObject* cls)
 #define LTE_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     LTE_DEF(scores), LTE_DEF(select_rule), LTE_DEF(attn_colsum), LTE_DEF(attn_prefill), LTE_DEF(cache_init), LTE_DEF(attn_decode),
-    LTE_DEF(attn_prefill_chunk), LTE_DEF(sparsity_stats), LTE_DEF(cache_score), LTE_DEF(attn_bwd),
+    LTE_DEF(attn_prefill_chunk), LTE_DEF(sparsity_stats), LTE_DEF(cache_score), LTE_DEF(attn_bwd), LTE_DEF(cache_init_accum), LTE_DEF(attn_decode_rows), LTE_DEF(cache4_convert),
     {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -140,6 +140,8 @@ int launch_decode_mma(const Params& p, void* cache, const void* q1, const void* 
                       cudaStream_t st);
 int launch_decode(const Params& p, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
                   float* lse1, cudaStream_t st);
+int launch_cache4_pack(const Params& p, const void* cache, void* cache4, cudaStream_t st);
+int launch_cache4_unpack(const Params& p, const void* cache4, void* cache, cudaStream_t st);
 size_t bwd_workspace_bytes(const Params& p, uint32_t flags);
 int launch_bwd(const Params& p, const void* q, const void* k, const void* v, const void* o, const float* lse,
                const void* dO, const float* z, const int32_t* idx, const int32_t* cnt, const float* lambda,

@@ -3,7 +3,7 @@
 
 #include <atomic>
 
-#include "common.cuh"
+#include "decode_rows.cuh"
 
 namespace lte {
 
@@ -100,6 +100,18 @@ int check_conv_or_stack(const lte_shape* s, const lte_conv* c)
         return LTE_OK;
     }
     return check_conv(s, c);
+}
+
+// shapes of the calls on caches that evict by accumulated attention or hold 4 bits
+int check_rows(const lte_shape* s)
+{
+    if (!s) return LTE_ERR_INVALID_ARG;
+    lte_shape one = *s;
+    one.T = 0;                                               // (ignored)
+    if (int e = check_shape(&one, false)) return e;
+    if ((long long)s->W + s->R > kRowsMost) return LTE_ERR_UNSUPPORTED;
+    if ((double)s->B * s->H * ((double)s->W + s->R) > 2.0e9) return LTE_ERR_UNSUPPORTED;   // blocks of a launch
+    return LTE_OK;
 }
 
 int check_arch()
@@ -434,6 +446,74 @@ int lte_attn_decode(const lte_shape* s, const lte_conv* c, void* cache, const vo
     if (!aligned16(cache) || !aligned16(q1) || !aligned16(k1) || !aligned16(v1)) return LTE_ERR_INVALID_ARG;
     e = check_arch(); if (e) return e;
     return launch_decode(make_params(s, c), cache, q1, k1, v1, o1, lse1, (cudaStream_t)stream);
+}
+
+int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const float* a, const int32_t* idx, const int32_t* cnt, void* cache,
+                         void* stream)
+{
+    int e = check_shape(s, false); if (e) return e;
+    e = check_rows(s); if (e) return e;
+    if (!cache || !aligned16(cache)) return LTE_ERR_INVALID_ARG;
+    if (s->T > 0 && (!k || !v || !a || !cnt || (s->R > 0 && !idx))) return LTE_ERR_INVALID_ARG;
+    if (!aligned(k, element_bytes(s)) || !aligned(v, element_bytes(s))) return LTE_ERR_INVALID_ARG;
+    e = check_arch(); if (e) return e;
+    return launch_cache_init(make_params(s, nullptr), k, v, a, idx, cnt, cache, (cudaStream_t)stream);   // (no token is unscored)
+}
+
+static int decode_rows(const lte_shape* s, const lte_conv* c, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1,
+                       const void* v1, void* o1, float* lse1, void* stream)
+{
+    int e = check_rows(s); if (e) return e;
+    if (accum) {
+        if (!(decay >= 0.f && decay <= 1.f)) return LTE_ERR_INVALID_ARG;
+    } else {
+        e = check_conv(s, c); if (e) return e;
+    }
+    if (!cache || !q1 || !k1 || !v1 || !o1 || !lse1) return LTE_ERR_INVALID_ARG;
+    if (!aligned16(cache) || !aligned16(q1) || !aligned16(k1) || !aligned16(v1) || !aligned(o1, element_bytes(s)) || !aligned(lse1, 4)) return LTE_ERR_INVALID_ARG;
+    e = check_arch(); if (e) return e;
+    return launch_decode_rows(make_params(s, c), four, accum, decay, cache, q1, k1, v1, o1, lse1, (cudaStream_t)stream);
+}
+
+int lte_attn_decode_accum(const lte_shape* s, float decay, void* cache, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
+                          void* stream)
+{
+    return decode_rows(s, nullptr, false, true, decay, cache, q1, k1, v1, o1, lse1, stream);
+}
+
+size_t lte_cache4_bytes(const lte_shape* s)
+{
+    if (check_rows(s) != LTE_OK) return 0;
+    const Cache4Layout L = cache4_layout(s->d, s->W, s->R);
+    return L.header + (size_t)s->B * s->H * L.stride;
+}
+
+int lte_cache4_pack(const lte_shape* s, const void* cache, void* cache4, void* stream)
+{
+    int e = check_rows(s); if (e) return e;
+    if (!cache || !cache4 || cache == cache4 || !aligned16(cache) || !aligned16(cache4)) return LTE_ERR_INVALID_ARG;
+    e = check_arch(); if (e) return e;
+    return launch_cache4_pack(make_params(s, nullptr), cache, cache4, (cudaStream_t)stream);
+}
+
+int lte_cache4_unpack(const lte_shape* s, const void* cache4, void* cache, void* stream)
+{
+    int e = check_rows(s); if (e) return e;
+    if (!cache || !cache4 || cache == cache4 || !aligned16(cache) || !aligned16(cache4)) return LTE_ERR_INVALID_ARG;
+    e = check_arch(); if (e) return e;
+    return launch_cache4_unpack(make_params(s, nullptr), cache4, cache, (cudaStream_t)stream);
+}
+
+int lte_attn_decode4(const lte_shape* s, const lte_conv* c, void* cache4, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
+                     void* stream)
+{
+    return decode_rows(s, c, true, false, 0.f, cache4, q1, k1, v1, o1, lse1, stream);
+}
+
+int lte_attn_decode4_accum(const lte_shape* s, float decay, void* cache4, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
+                           void* stream)
+{
+    return decode_rows(s, nullptr, true, true, decay, cache4, q1, k1, v1, o1, lse1, stream);
 }
 
 int lte_sparsity_stats(const lte_shape* s, const float* z, const float* lambda_or_null, float* count, float* penalty,

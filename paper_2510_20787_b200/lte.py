@@ -24,7 +24,8 @@ RULE_LEARNED, RULE_UNIFORM, RULE_ACCUM_ATTN = 0, 1, 2
 
 EXPORTS = ["lte_device_status", "lte_workspace_bytes", "lte_strerror", "lte_scores", "lte_select", "lte_cache_score", "lte_attn_prefill",
            "lte_cache_bytes", "lte_cache_init", "lte_attn_decode", "lte_attn_prefill_chunk", "lte_attn_bwd", "lte_attn_bwd_static",
-           "lte_sparsity_stats", "lte_lambda_update", "lte_cache_score_unrope", "lte_selftest_per_device", "lte_select_rule", "lte_attn_colsum", "lte_attn_prefill_chunk_ex"]
+           "lte_sparsity_stats", "lte_lambda_update", "lte_cache_score_unrope", "lte_selftest_per_device", "lte_select_rule", "lte_attn_colsum", "lte_attn_prefill_chunk_ex",
+           "lte_cache_init_accum", "lte_attn_decode_accum", "lte_cache4_bytes", "lte_cache4_pack", "lte_cache4_unpack", "lte_attn_decode4", "lte_attn_decode4_accum"]
 STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -78,8 +79,14 @@ def lib():
         L.lte_selftest_per_device.argtypes = [ctypes.c_int]
         L.lte_select_rule.argtypes = [vp, ctypes.c_int] + [vp] * 5 + [ctypes.c_size_t, vp]
         L.lte_attn_colsum.argtypes = [vp] * 8
+        L.lte_cache_init_accum.argtypes = [vp] * 8
+        L.lte_attn_decode_accum.argtypes = L.lte_attn_decode4_accum.argtypes = [vp, ctypes.c_float] + [vp] * 7
+        L.lte_cache4_bytes.restype = ctypes.c_size_t
+        L.lte_cache4_bytes.argtypes = [vp]
+        L.lte_cache4_pack.argtypes = L.lte_cache4_unpack.argtypes = [vp] * 4
+        L.lte_attn_decode4.argtypes = [vp] * 9
         for name in EXPORTS:
-            if name not in ("lte_strerror", "lte_workspace_bytes", "lte_cache_bytes", "lte_device_status"):
+            if name not in ("lte_strerror", "lte_workspace_bytes", "lte_cache_bytes", "lte_cache4_bytes", "lte_device_status"):
                 getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -194,6 +201,57 @@ def lte_attn_decode(s, c, cache, q1, k1, v1, o1=None, lse1=None):
     """One decode step: q1 [B,H*group,d], k1, v1 [B,H,d] -> o1 [B,H*group,d], lse1 [B,H*group]; the cache is
     updated in place."""
     return (_native or _load()).attn_decode(s, c, cache, q1, k1, v1, o1, lse1)
+
+
+def _new_cache(n, s, like):
+    if n == 0:
+        raise LteError("lte_cache_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=like.device if like is not None else torch.device("cuda"))
+
+
+def lte_cache_init_accum(s, k=None, v=None, a=None, idx=None, cnt=None, cache=None):
+    """Decode cache whose rows are ranked by accumulated attention: a [B,H,T] fp32 of lte_attn_colsum, the list of
+    lte_select_rule(RULE_ACCUM_ATTN) (T = 0: empty cache)."""
+    if cache is None:
+        cache = _new_cache(lte_cache_bytes(s), s, k)
+    return (_native or _load()).cache_init_accum(s, k, v, a, idx, cnt, cache)
+
+
+def lte_attn_decode_accum(s, cache, q1, k1, v1, decay=1.0, o1=None, lse1=None):
+    """One decode step under eviction by accumulated attention: q1 [B,H*group,d], k1, v1 [B,H,d] -> o1 [B,H*group,d], lse1
+    [B,H*group]; the cache of lte_cache_init_accum is updated in place, its scores to decay * score + this step's weights."""
+    return (_native or _load()).attn_decode_rows(s, None, float(decay), cache, q1, k1, v1, o1, lse1, False)
+
+
+def lte_cache4_bytes(s):
+    """Bytes of a cache in 4 bits; 0 for a shape that the calls refuse."""
+    return int(lib().lte_cache4_bytes(ctypes.addressof(s)))
+
+
+def lte_cache4_pack(s, cache, cache4=None):
+    """An ordinary cache (lte_cache_init, lte_cache_init_accum) rounded to 4 bits."""
+    if cache4 is None:
+        cache4 = _new_cache(lte_cache4_bytes(s), s, cache)
+    return (_native or _load()).cache4_convert(s, cache, cache4, True)
+
+
+def lte_cache4_unpack(s, cache4, cache=None):
+    """A cache in 4 bits as an ordinary one of s.dtype, e.g. for lte_attn_prefill_chunk."""
+    if cache is None:
+        cache = _new_cache(lte_cache_bytes(s), s, cache4)
+    return (_native or _load()).cache4_convert(s, cache4, cache, False)
+
+
+def lte_attn_decode4(s, c, cache4, q1, k1, v1, o1=None, lse1=None):
+    """lte_attn_decode over a cache in 4 bits (single-layer scorer)."""
+    if c is None:
+        raise TypeError("lte_attn_decode4 needs a scorer; under accumulated attention: lte_attn_decode4_accum")
+    return (_native or _load()).attn_decode_rows(s, c, 0.0, cache4, q1, k1, v1, o1, lse1, True)
+
+
+def lte_attn_decode4_accum(s, cache4, q1, k1, v1, decay=1.0, o1=None, lse1=None):
+    """lte_attn_decode_accum over a cache in 4 bits."""
+    return (_native or _load()).attn_decode_rows(s, None, float(decay), cache4, q1, k1, v1, o1, lse1, True)
 
 
 def lte_attn_prefill_chunk(s, c, cache, n_past, q, k, v, o=None, lse=None, ws=None, streaming=False):
