@@ -27,7 +27,7 @@
 // ring's rows in L2 ahead of the grid dependency made the large shapes slower (4 and 13 %).
 #include <cooperative_groups.h>
 
-#include "common.cuh"
+#include "row_mma.cuh"
 
 namespace lte {
 namespace cg = cooperative_groups;
@@ -39,26 +39,6 @@ constexpr float M_NONE = -1e30f;                                // a reference b
 __host__ __device__ constexpr int warps_per_sm(int d) { return d == 128 ? 8 : 16; }
 __host__ __device__ constexpr int max_warps(int d) { return d == 128 ? 4 : 8; }
 constexpr int MAX_SPLIT = 8;                                   // blocks per head
-
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
 // Up to 16 consecutive rows of the ring or of the pool, or the incoming token alone (row = -1).
 struct Span { int row, n; };

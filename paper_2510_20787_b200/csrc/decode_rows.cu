@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
                 for (int g = 0; g < nq; ++g) a += f[g] * s_log[u * nq + g];
                 if (G > QP) { a += g0 > 0 ? s_sum[u] : 0.f; s_sum[u] = a; }
                 const int row = row_of(u);
-                if (last && seen(row)) zc[row == slot && p >= 0 ? W + dst : row] = rule.decay * zc[row] + a;
+                if (last && seen(row)) zc[row == slot && p >= 0 ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, zc[row], a) : a;
             }
             if (rank == 0 && tid == 0) {
                 float a = g0 > 0 ? s_tap[0] : 0.f;
@@ -319,6 +319,9 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
 int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
                        float* lse1, cudaStream_t st)
 {
+    const RowsRule rule = {decay, p.zthr, p.K, p.w, p.bias};
+    if (p.dtype == LTE_BF16)
+        return four ? launch_decode_rows4_bf16(p, accum, rule, cache, q1, k1, v1, o1, lse1, st) : launch_decode_rows_bf16(p, rule, cache, q1, k1, v1, o1, lse1, st);
     const CacheLayout C = cache_layout(p.d, p.W, p.R, p.dtype);
     const RowsLayout L = four ? rows_layout(cache4_layout(p.d, p.W, p.R)) : rows_layout(C);
     int n_sm = 0;
@@ -327,7 +330,6 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
     auto smem = [&](int split) { return (size_t)((rows + split - 1) / split) * (nq + (p.G > QP ? 1 : 0)) * 4; };
     int nsplit = 1;
     while (nsplit < MAX_SPLIT && (smem(nsplit) > 48 * 1024 || (BH * nsplit * 2 <= 2 * n_sm && rows / (nsplit * 2) >= 32))) nsplit *= 2;
-    const RowsRule rule = {decay, p.zthr, p.K, p.w, p.bias};
     auto go = [&](auto t, auto d, auto f4, auto acc) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
@@ -357,7 +359,7 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
         }
         return (int)LTE_ERR_UNSUPPORTED;
     };
-    return p.dtype == LTE_BF16 ? dims(__nv_bfloat16()) : dims(0.f);
+    return dims(0.f);
 }
 
 }  // namespace lte

@@ -40,6 +40,10 @@ struct Worst {
     }
 };
 
+int launch_decode_rows_bf16(const Params& p, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
+                            cudaStream_t st);
+int launch_decode_rows4_bf16(const Params& p, bool accum, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
+                             float* lse1, cudaStream_t st);
 int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
                        float* lse1, cudaStream_t st);
 

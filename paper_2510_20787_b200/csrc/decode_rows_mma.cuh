@@ -1,0 +1,721 @@
+// Decode step (lte_attn_decode_accum, lte_attn_decode4, lte_attn_decode4_accum) for bf16 calls: rows go from memory straight into tensor-core
+// operands, as in decode_mma.cu, every query head of a group at once, heads split over warps and clusters where there are few.
+//
+// Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there unpacking and memory are about even.  Every warp
+// walks spans of 16 rows (interleaved over the warps of all blocks that share the head) with NBUF spans in flight, keeps its own
+// reference, sum and output, and meets the others once at the end.  The incoming token is no row: its logit is a dot product on the fp32 ALUs, and it
+// joins where the warps meet.
+//
+// Scores (accumulated attention): a row's weight needs the sum over all rows, so the raw logits of a warp's rows stay in shared memory until the
+// blocks have met; then every warp adds its rows' weights, summed over the query heads, to their scores.  One read and one write of 4 bytes a row.
+//
+// Products are mma.sync m16n8k16: logits S^T[16 rows][8 queries] = K q^T, output O^T[16 channels][8 queries] += V^T P^T, N = 8 queries.
+// Rows in 4 bits.  A code c < 16 becomes the bf16 number 1 + c / 16 by a shift and one three-input logic operation on two codes at a time (the
+// code is the top of the mantissa): exact, no conversion.  With value = zero + c step = (zero - 16 step) + 16 step (1 + c / 16):
+//   logits   per group of 32 channels, 16 step (1 + c/16).q + (zero - 16 step) sum(q): the group's product starts from zero, and its two
+//            scalars, which belong to a row, are applied to the products in fp32 (a lane holds rows g and g + 8 of both);
+//   output   P 16 step takes the place of P, per group, and P (zero - 16 step), which is the same for all channels of a group, is summed beside it.
+// The contraction index may be permuted freely: the nibbles i and i + 4 of a key word are neighbours in it, and so are the two rows whose value
+// units a byte permute joins.  The order of the codes in the cache (cache4.cuh) makes these the words that a lane loads.
+// P (times 16 step) is split into two bf16 terms: 16 bits of mantissa.  With one term o would be off by more than its own rounding: the 1 + c/16
+// are all positive, so that o is the small difference of sums as large as the rows.
+#pragma once
+#include <cfloat>
+#include <cooperative_groups.h>
+
+#include <type_traits>
+
+#include "decode_rows.cuh"
+#include "row_mma.cuh"
+
+namespace lte {
+namespace cg = cooperative_groups;
+namespace {
+
+constexpr int MQ = 8;                                          // query heads per pass
+__host__ __device__ constexpr int warps_per_sm(int d) { return d == 128 ? 8 : 16; }   // resident warps the registers are budgeted for
+__host__ __device__ constexpr int max_warps(int d) { return d == 128 ? 4 : 8; }       // per block
+constexpr int MAX_SPLIT = 8;                                   // blocks per head
+
+struct Span { int row, n; };                                   // up to 16 consecutive rows of the ring or of the pool
+struct Rows {
+    const unsigned char *K, *V, *KP, *VP;
+    int n_ring, cnt, W, ring_spans, spans;
+    __device__ __forceinline__ Span span(int i) const
+    {
+        const bool ring = i < ring_spans;
+        const int at = (ring ? i : i - ring_spans) << 4;
+        return {ring ? at : W + at, min(16, (ring ? n_ring : cnt) - at)};
+    }
+};
+
+// What a lane (g, t) = (lane / 4, lane % 4) holds of a span's 16 rows, and the two products with it.  Rows past the end of a span repeat its
+// last row; they and the rows that the step leaves out have weight zero, and what they hold is cleared (zero times an infinite value is NaN).
+template <int D, bool SWZ, bool FOUR> struct Group;
+
+template <int D, bool SWZ> struct Group<D, SWZ, false> {
+    static constexpr int KP = D / 32, VB = D / 16, PITCH = D * 2, MT = D / 16, GR = 0;
+    uint4 k[2][KP];                                            // pieces t, t + 4, .. of rows g, g + 8
+    uint32_t v[4][VB];                                         // pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9
+    struct Query { uint4 f[KP]; };                             // pieces t, t + 4, .. of query g
+    struct Acc { float a[MT][4]; };
+    static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
+    {
+#pragma unroll
+        for (int j = 0; j < KP; ++j) Q.f[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void load_k(const Rows& R, const Span& s, int g, int t)
+    {
+        const unsigned char* base = R.K + (size_t)s.row * PITCH;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1), sw = SWZ ? (s.row + r) & 7 : 0;
+            const unsigned char* p = base + r * PITCH;
+#pragma unroll
+            for (int j = 0; j < KP; ++j) k[i][j] = *reinterpret_cast<const uint4*>(p + (((t + 4 * j) ^ sw) << 4));
+        }
+    }
+    __device__ __forceinline__ void load_v(const Rows& R, const Span& s, int g, int t)
+    {
+        const unsigned char* base = R.V + (size_t)s.row * PITCH;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int ri = 2 * t + (i & 1) + 8 * (i >> 1), r = s.n == 16 ? ri : min(ri, s.n - 1), sw = SWZ ? (s.row + r) & 7 : 0;
+            const unsigned char* p = base + r * PITCH;
+            if constexpr (D == 32) {
+                const uint2 u = *reinterpret_cast<const uint2*>(p + (g << 3));
+                v[i][0] = u.x; v[i][1] = u.y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(p + (((g + 8 * j) ^ sw) << 4));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[i][4 * j + w] = word(u, w);
+                }
+            }
+        }
+    }
+    // c: rows g (0, 1) and g + 8 (2, 3), queries 2t and 2t + 1.  A product rounds its running sum towards zero, so every one starts from zero
+    // and the parts are added to the nearest (see decode_mma.cu).
+    __device__ __forceinline__ void logits(float (&c)[4], const Query& Q) const
+    {
+        constexpr int NS = D == 128 ? 2 * KP : 1;
+        float cs[NS][4];
+#pragma unroll
+        for (int i = 0; i < 2 * KP; ++i) {
+            const int j = i >> 1, s = 2 * (i & 1);
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            mma16816(part, word(k[0][j], s), word(k[1][j], s), word(k[0][j], s + 1), word(k[1][j], s + 1), word(Q.f[j], s), word(Q.f[j], s + 1));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[i % NS][e] = i < NS ? part[e] : cs[i % NS][e] + part[e];
+        }
+#pragma unroll
+        for (int w = NS / 2; w > 0; w >>= 1)
+#pragma unroll
+            for (int j = 0; j < w; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cs[j][e] += cs[j + w][e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = cs[0][e];
+    }
+    template <typename F> __device__ __forceinline__ void clear(F&& out, int, int t)         // rows of the span that out(row) names
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (out(2 * t + (i & 1) + 8 * (i >> 1)))
+#pragma unroll
+                for (int j = 0; j < VB; ++j) v[i][j] = 0u;
+    }
+    static __device__ __forceinline__ void start(Acc& A)
+    {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) A.a[m][0] = A.a[m][1] = A.a[m][2] = A.a[m][3] = 0.f;
+    }
+    static __device__ __forceinline__ void rescale(Acc& A, float f0, float f1)
+    {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
+    }
+    __device__ __forceinline__ void output(Acc& A, float p0, float p1, float p2, float p3) const
+    {
+        const uint32_t hi0 = pack_bf16(p0, p1), hi1 = pack_bf16(p2, p3);
+        const uint32_t lo0 = pack_bf16(p0 - __uint_as_float(hi0 << 16), p1 - __uint_as_float(hi0 & 0xffff0000u));
+        const uint32_t lo1 = pack_bf16(p2 - __uint_as_float(hi1 << 16), p3 - __uint_as_float(hi1 & 0xffff0000u));
+        const uint32_t h0 = movmatrix_trans(hi0), h1 = movmatrix_trans(hi1), e0 = movmatrix_trans(lo0), e1 = movmatrix_trans(lo1);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint32_t a0 = __byte_perm(v[0][m], v[1][m], 0x5410), a1 = __byte_perm(v[0][m], v[1][m], 0x7632);
+            const uint32_t a2 = __byte_perm(v[2][m], v[3][m], 0x5410), a3 = __byte_perm(v[2][m], v[3][m], 0x7632);
+            mma16816(A.a[m], a0, a1, a2, a3, h0, h1);
+            mma16816(A.a[m], a0, a1, a2, a3, e0, e1);
+        }
+    }
+    static __device__ __forceinline__ void finish(Acc&) {}
+    static __device__ __forceinline__ int channel(int m, int g) { return D == 32 ? g * 4 + 2 * m : (m >> 2) * 64 + g * 8 + 2 * (m & 3); }
+};
+
+// two codes of a word, at bits 4i and 4i + 16, as the bf16 numbers 1 + c / 16
+template <int I> __device__ __forceinline__ uint32_t codes2(uint32_t x)
+{
+    const uint32_t y = I == 0 ? x << 3 : x >> (4 * I - 3);
+    return (y & 0x00780078u) | 0x3f803f80u;
+}
+
+template <int D, bool SWZ> struct Group<D, SWZ, true> {
+    static constexpr int GR = D / kGroup4, MT = D / 16;
+    uint32_t k[2][GR], kp[2][GR], v[4][(GR + 1) / 2], vp[2][GR];   // of rows g, g + 8 (values: units g of rows 2t, 2t + 1, 2t + 8, 2t + 9)
+    struct Query { uint32_t f[GR][4]; float sum[GR][2]; };     // of query g; sums of queries 2t, 2t + 1 over a group's channels
+    struct Acc { float a[MT][4], z[GR][2]; };
+    template <typename U> static __device__ __forceinline__ void get(uint32_t (&x)[GR], const unsigned char* p)
+    {
+        const U u = *reinterpret_cast<const U*>(p);
+        memcpy(x, &u, sizeof(U));
+    }
+    using Words = std::conditional_t<GR == 1, uint32_t, std::conditional_t<GR == 2, uint2, uint4>>;
+    using Units = std::conditional_t<GR == 1, uint16_t, std::conditional_t<GR == 2, uint32_t, uint2>>;
+    static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
+    {
+        const int lane = 4 * g + t;
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+            const uint4 u = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D + j * kGroup4)[t] : make_uint4(0, 0, 0, 0);
+            Q.f[j][0] = __byte_perm(u.x, u.z, 0x5410); Q.f[j][1] = __byte_perm(u.x, u.z, 0x7632);   // channels 0, 4 | 1, 5
+            Q.f[j][2] = __byte_perm(u.y, u.w, 0x5410); Q.f[j][3] = __byte_perm(u.y, u.w, 0x7632);   // 2, 6 | 3, 7
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s += __uint_as_float(word(u, w) << 16) + __uint_as_float(word(u, w) & 0xffff0000u);
+            s += __shfl_xor_sync(0xffffffffu, s, 1);
+            s += __shfl_xor_sync(0xffffffffu, s, 2);
+            Q.sum[j][0] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3));
+            Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3) + 4);
+        }
+    }
+    __device__ __forceinline__ void load_k(const Rows& R, const Span& s, int g, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1);
+            get<Words>(k[i], R.K + (size_t)s.row * (D / 2) + r * (D / 2) + t * (4 * GR));
+            get<Words>(kp[i], R.KP + (size_t)s.row * (4 * GR) + r * (4 * GR));
+        }
+    }
+    __device__ __forceinline__ void load_v(const Rows& R, const Span& s, int g, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int ri = 2 * t + (i & 1) + 8 * (i >> 1), r = s.n == 16 ? ri : min(ri, s.n - 1);
+            const Units u = *reinterpret_cast<const Units*>(R.V + (size_t)s.row * (D / 2) + r * (D / 2) + g * (2 * GR));
+            if constexpr (GR == 1) v[i][0] = u;
+            else memcpy(v[i], &u, sizeof(u));
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1);
+            get<Words>(vp[i], R.VP + (size_t)s.row * (4 * GR) + r * (4 * GR));
+        }
+    }
+    __device__ __forceinline__ void logits(float (&c)[4], const Query& Q) const
+    {
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+            float p[4] = {0.f, 0.f, 0.f, 0.f};
+            mma16816(p, codes2<0>(k[0][j]), codes2<0>(k[1][j]), codes2<1>(k[0][j]), codes2<1>(k[1][j]), Q.f[j][0], Q.f[j][1]);
+            mma16816(p, codes2<2>(k[0][j]), codes2<2>(k[1][j]), codes2<3>(k[0][j]), codes2<3>(k[1][j]), Q.f[j][2], Q.f[j][3]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float s16 = 16.f * par4_step(kp[i][j]), z16 = par4_zero(kp[i][j]) - s16;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float x = z16 * Q.sum[j][e];
+                    c[2 * i + e] = j == 0 ? fmaf(s16, p[2 * i + e], x) : c[2 * i + e] + fmaf(s16, p[2 * i + e], x);
+                }
+            }
+        }
+    }
+    template <typename F> __device__ __forceinline__ void clear(F&& out, int g, int)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (out(g + 8 * i))
+#pragma unroll
+                for (int j = 0; j < GR; ++j) vp[i][j] = 0u;
+    }
+    static __device__ __forceinline__ void start(Acc& A)
+    {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) A.a[m][0] = A.a[m][1] = A.a[m][2] = A.a[m][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < GR; ++j) A.z[j][0] = A.z[j][1] = 0.f;
+    }
+    static __device__ __forceinline__ void rescale(Acc& A, float f0, float f1)
+    {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
+#pragma unroll
+        for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
+    }
+    __device__ __forceinline__ void output(Acc& A, float p0, float p1, float p2, float p3) const
+    {
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+            const float s0 = 16.f * par4_step(vp[0][j]), s1 = 16.f * par4_step(vp[1][j]);
+            const float z0 = par4_zero(vp[0][j]) - s0, z1 = par4_zero(vp[1][j]) - s1;
+            A.z[j][0] = fmaf(p2, z1, fmaf(p0, z0, A.z[j][0]));
+            A.z[j][1] = fmaf(p3, z1, fmaf(p1, z0, A.z[j][1]));
+            const float x0 = p0 * s0, x1 = p1 * s0, x2 = p2 * s1, x3 = p3 * s1;
+            const uint32_t hi0 = pack_bf16(x0, x1), hi1 = pack_bf16(x2, x3);
+            const uint32_t lo0 = pack_bf16(x0 - __uint_as_float(hi0 << 16), x1 - __uint_as_float(hi0 & 0xffff0000u));
+            const uint32_t lo1 = pack_bf16(x2 - __uint_as_float(hi1 << 16), x3 - __uint_as_float(hi1 & 0xffff0000u));
+            const uint32_t h0 = movmatrix_trans(hi0), h1 = movmatrix_trans(hi1), e0 = movmatrix_trans(lo0), e1 = movmatrix_trans(lo1);
+            const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410);   // four codes of row 2t, of row 2t + 1
+            const uint32_t w = __byte_perm(v[2][j / 2], v[3][j / 2], j & 1 ? 0x7632 : 0x5410);
+            mma16816(A.a[2 * j], codes2<0>(u), codes2<1>(u), codes2<0>(w), codes2<1>(w), h0, h1);
+            mma16816(A.a[2 * j], codes2<0>(u), codes2<1>(u), codes2<0>(w), codes2<1>(w), e0, e1);
+            mma16816(A.a[2 * j + 1], codes2<2>(u), codes2<3>(u), codes2<2>(w), codes2<3>(w), h0, h1);
+            mma16816(A.a[2 * j + 1], codes2<2>(u), codes2<3>(u), codes2<2>(w), codes2<3>(w), e0, e1);
+        }
+    }
+    // the groups' constant parts, summed over the lanes of a query, into the outputs (of one lane's rows each: lanes g = 0)
+    static __device__ __forceinline__ void finish(Acc& A)
+    {
+#pragma unroll
+        for (int j = 0; j < GR; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float z = A.z[j][e];
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+                A.a[2 * j][e] += z; A.a[2 * j][2 + e] += z; A.a[2 * j + 1][e] += z; A.a[2 * j + 1][2 + e] += z;
+            }
+    }
+    static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
+};
+
+template <int D, int NW, bool SWZ, bool FOUR, bool ACCUM>
+__global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma_kernel(
+    unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
+    const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
+    float scale, int G, int most)                              // most: rows whose logits a warp keeps (whole spans)
+{
+    using Gr = Group<D, SWZ, FOUR>;
+    constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
+    constexpr int NBUF = FOUR ? 3 : 2;                         // spans in flight per warp
+    constexpr int SPLIT = NW == max_warps(D) ? MAX_SPLIT : 1;  // (only the largest blocks come in clusters)
+    extern __shared__ __align__(16) float s_log[];             // [NW][most][nq], behind them [NW][most] sums over passes
+    __shared__ __align__(16) float s_acc[NW][MQ][PITCH];
+    __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
+    __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
+    __shared__ __align__(16) float s_ml[2][SPLIT][MQ][2];      // the cluster's shares of this block's output elements (by pass parity)
+    __shared__ __align__(16) __nv_bfloat16 s_kv[2][D];         // the incoming token
+    __shared__ float s_tap[kMaxTaps];
+    __shared__ uint32_t s_wkey[NW];
+    __shared__ int s_wpos[NW], s_wslot[NW];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int nsplit = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int bh = blockIdx.x / nsplit, h = bh % H;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
+    unsigned char* blk = cache + L.header + (size_t)bh * L.stride;
+    float* zc = reinterpret_cast<float*>(blk + L.off_z);
+    int32_t* pidx = reinterpret_cast<int32_t*>(blk + L.off_pidx);
+    int32_t* meta = reinterpret_cast<int32_t*>(blk + L.off_meta);
+    const bool shared_head = SPLIT > 1 && nsplit > 1;          // (uniform in the cluster)
+    if (shared_head) cluster.barrier_arrive();                 // (awaited before the first store into another block's shared memory)
+    pdl_launch_dependents();
+    pdl_wait();
+
+    // Everything whose address is known is asked for at once, then everything that needs the counters.
+    const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
+    typename Gr::Query qf;
+    Gr::load_q(qf, q1 + (size_t)bh * G * D, g < G, g, t);
+    constexpr int PRE = NT < 256 ? 4 : 2;                      // scores and positions of the pool, before it is known whether the decision needs them
+    float pz[PRE];
+    int pp[PRE];
+#pragma unroll
+    for (int u = 0; u < PRE; ++u) {
+        const int m = tid + u * NT;
+        pz[u] = m < R ? zc[W + m] : INFINITY;
+        pp[u] = m < R ? pidx[m] : -1;
+    }
+    if (tid < D / 4) reinterpret_cast<uint4*>(s_kv)[tid] = reinterpret_cast<const uint4*>((tid < D / 8 ? k1 : v1) + (size_t)bh * D)[tid % (D / 8)];
+    float wk[CPL], wv[CPL];                                    // scorer weights of tap `wid` (the first block scores)
+    const bool taps = !ACCUM && rank == 0 && wid < rule.K;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) {
+        wk[c] = taps ? rule.w[((size_t)h * rule.K + wid) * 2 * D + lane + 32 * c] : 0.f;
+        wv[c] = taps ? rule.w[((size_t)h * rule.K + wid) * 2 * D + D + lane + 32 * c] : 0.f;
+    }
+    const int slot = n % W, p = n - W, half = rule.K / 2;
+    Rows rows;
+    rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
+    rows.W = W; rows.cnt = cnt_old;
+    rows.n_ring = min(n, W);
+    rows.ring_spans = (rows.n_ring + 15) >> 4;
+    rows.spans = rows.ring_spans + ((cnt_old + 15) >> 4);
+    const int step = NW * nsplit, first = wid * nsplit + rank;
+    auto has = [&](int i) { return i < rows.spans; };
+    Gr buf[NBUF];
+    const float zp = p >= 0 ? zc[slot] : 0.f;
+#pragma unroll
+    for (int b = 0; b < NBUF; ++b)
+        if (has(first + b * step)) { const Span sp = rows.span(first + b * step); buf[b].load_k(rows, sp, g, t); buf[b].load_v(rows, sp, g, t); }
+    // learned rule: channels lane, lane + 32, .. of the row under a tap, as the cache holds it
+    const int jsc = ACCUM ? -1 : n - half;
+    auto tap_rows = [&](int tap, float (&kx)[CPL], float (&vx)[CPL]) {
+        const int pos = jsc + tap - half, r = pos < 0 ? 0 : pos % W;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            kx[c] = vx[c] = 0.f;
+            if (pos == n) {
+                kx[c] = __bfloat162float(k1[(size_t)bh * D + lane + 32 * c]);
+                vx[c] = __bfloat162float(v1[(size_t)bh * D + lane + 32 * c]);
+            } else if (pos >= 0) {
+                const uint32_t kw = reinterpret_cast<const uint32_t*>(rows.K + (size_t)r * (D / 2))[(lane >> 3) * GR + c];
+                const uint32_t vw = reinterpret_cast<const uint16_t*>(rows.V + (size_t)r * (D / 2))[(lane >> 2) * GR + c];
+                kx[c] = value4((kw >> (4 * (lane & 7))) & 15u, reinterpret_cast<const uint32_t*>(rows.KP)[(size_t)r * GR + c]);
+                vx[c] = value4((vw >> (4 * (lane & 3))) & 15u, reinterpret_cast<const uint32_t*>(rows.VP)[(size_t)r * GR + c]);
+            }
+        }
+    };
+    float kx[CPL], vx[CPL];
+    if (taps && jsc >= 0) tap_rows(wid, kx, vx);
+
+    // ---- what happens to the token leaving the window ------------------------------------------------------------
+    int dst = -1, cnt_new = cnt_old;
+    if (p >= 0 && R > 0 && (ACCUM || p < sink || zp > rule.zthr)) {
+        if (cnt_old < R) { dst = cnt_old; cnt_new = cnt_old + 1; }
+        else if (p >= sink) {
+            Worst w;
+#pragma unroll
+            for (int u = 0; u < PRE; ++u) if (tid + u * NT < cnt_old) w.offer(pz[u], pp[u], tid + u * NT, sink);
+            for (int m = tid + PRE * NT; m < cnt_old; m += NT) w.offer(zc[W + m], pidx[m], m, sink);
+            w.over_warp();
+            if (NW > 1) {
+                if (lane == 0) { s_wkey[wid] = w.key; s_wpos[wid] = w.pos; s_wslot[wid] = w.slot; }
+                __syncthreads();
+                w.key = lane < NW ? s_wkey[lane] : 0xffffffffu; w.pos = lane < NW ? s_wpos[lane] : -1; w.slot = lane < NW ? s_wslot[lane] : -1;
+                w.over_warp();
+            }
+            if (w.slot >= 0 && order_key(zp + 0.f) > w.key) dst = w.slot;
+        }
+    }
+    const int masked_ring = p >= 0 && dst < 0 ? slot : -32;    // the popped row counts iff the pool takes it ...
+    const int masked_pool = dst >= 0 && dst < cnt_old ? W + dst : -32;   // ... and then the entry it replaces does not
+
+    // ---- learned rule, the first block: logit of the newest token whose receptive field is complete -----------------
+    if (!ACCUM && rank == 0 && jsc >= 0) {
+        for (int tap = wid; tap < rule.K; tap += NW) {
+            if (tap >= NW) {
+                tap_rows(tap, kx, vx);
+#pragma unroll
+                for (int c = 0; c < CPL; ++c) {
+                    wk[c] = rule.w[((size_t)h * rule.K + tap) * 2 * D + lane + 32 * c];
+                    wv[c] = rule.w[((size_t)h * rule.K + tap) * 2 * D + D + lane + 32 * c];
+                }
+            }
+            float a = 0.f;
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) a += wk[c] * kx[c] + wv[c] * vx[c];
+            a = warp_sum(a);
+            if (lane == 0) s_tap[tap] = a;
+        }
+    }
+
+    // the popped row's words, read before the slot is written: thread e of the last ones moves word e
+    constexpr int WORDS = FOUR ? 2 * (D / 8 + GR) : 2 * (D / 8), MOVES = (WORDS + NT - 1) / NT;   // (bf16: 16-byte pieces)
+    using Move = std::conditional_t<FOUR, uint32_t, uint4>;
+    auto place = [&](int e, int row) -> Move* {                // word e of a row's keys, key parameters, values, value parameters
+        if constexpr (FOUR) {
+            constexpr int P = D / 8 + GR;
+            const bool values = e >= P;
+            const int w = e - (values ? P : 0);
+            return reinterpret_cast<uint32_t*>(blk + (w < D / 8 ? (values ? L.off_v : L.off_k) : (values ? L.off_vp : L.off_kp)))
+                   + (w < D / 8 ? (size_t)row * (D / 8) + w : (size_t)row * GR + (w - D / 8));
+        } else {
+            const int c = e % (D / 8);
+            return reinterpret_cast<uint4*>(blk + (e < D / 8 ? L.off_k : L.off_v)) + (size_t)row * (D / 8) + (SWZ ? c ^ (row & 7) : c);
+        }
+    };
+    Move mv[MOVES];
+
+    const float scale2 = scale * 1.44269504088896340736f, jump = 8.f / scale2;   // jump: a factor of 2^8 between weights, unscaled
+    const int nqs = min(G, MQ);                                // logits kept per row
+    float* wlog = s_log + (size_t)wid * most * nqs;            // this warp's
+    float* wsum = s_log + (size_t)NW * most * nqs + (size_t)wid * most;
+    float fresh = 0.f;                                         // the incoming token's weights (thread 0 of the first block)
+    for (int g0 = 0; g0 < G; g0 += MQ) {
+        const int nq = min(MQ, G - g0);
+        if (g0 > 0) {                                          // further query heads read the rows again
+            Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
+#pragma unroll
+            for (int b = 0; b < NBUF; ++b)
+                if (has(first + b * step)) { const Span sp = rows.span(first + b * step); buf[b].load_k(rows, sp, g, t); buf[b].load_v(rows, sp, g, t); }
+        }
+        typename Gr::Acc acc;
+        Gr::start(acc);
+        float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
+        int kept = 0;                                          // rows whose logits this warp has kept
+
+        // one span; its registers are refilled with the warp's span NBUF steps ahead as soon as a product has taken them
+        auto compute = [&](Gr& u, int i) {
+            const Span cur = rows.span(i), nxt = rows.span(i + NBUF * step);
+            const bool more = has(i + NBUF * step);
+            float c[4];
+            u.logits(c, qf);
+            if (more) u.load_k(rows, nxt, g, t);
+            if (cur.n < 16 || (unsigned)(masked_ring - cur.row) < 16u || (unsigned)(masked_pool - cur.row) < 16u) {
+                auto out = [&](int r) { return r >= cur.n || cur.row + r == masked_ring || cur.row + r == masked_pool; };
+                if (out(g)) c[0] = c[1] = -INFINITY;
+                if (out(g + 8)) c[2] = c[3] = -INFINITY;
+                u.clear(out, g, t);
+            }
+            if constexpr (ACCUM) {                             // raw logits [row][query]
+                float* at = wlog + (size_t)(kept + g) * nq + 2 * t;
+                if (2 * t < nq) { at[0] = c[0]; at[8 * nq] = c[2]; }
+                if (2 * t + 1 < nq) { at[1] = c[1]; at[8 * nq + 1] = c[3]; }
+                kept += 16;
+            }
+            // The reference m follows the maximum only when that has grown by 2^8 (weights stay below 2^8, in fp32): a vote per
+            // span instead of a reduction over its rows.
+            const float x0 = fmaxf(c[0], c[2]), x1 = fmaxf(c[1], c[3]);
+            if (__any_sync(0xffffffffu, x0 > m0 + jump || x1 > m1 + jump)) {
+                float y0 = x0, y1 = x1;
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, o));
+                    y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, o));
+                }
+                y0 = fmaxf(y0, m0); y1 = fmaxf(y1, m1);
+                const float f0 = exp2_fast((m0 - y0) * scale2), f1 = exp2_fast((m1 - y1) * scale2);
+                m0 = y0; m1 = y1;
+                l0 *= f0; l1 *= f1;
+                Gr::rescale(acc, f0, f1);
+            }
+            const float p0 = exp2_fast((c[0] - m0) * scale2), p1 = exp2_fast((c[1] - m1) * scale2);
+            const float p2 = exp2_fast((c[2] - m0) * scale2), p3 = exp2_fast((c[3] - m1) * scale2);
+            l0 += p0 + p2; l1 += p1 + p3;
+            u.output(acc, p0, p1, p2, p3);
+            if (more) u.load_v(rows, nxt, g, t);
+        };
+        for (int i = first; has(i); i += NBUF * step) {
+#pragma unroll
+            for (int b = 0; b < NBUF; ++b)
+                if (has(i + b * step)) compute(buf[b], i + b * step);
+        }
+        const bool last = g0 + MQ >= G;
+        if (rank == 0 && last && dst >= 0)                     // (back by the time the write-back needs them)
+#pragma unroll
+            for (int u = 0; u < MOVES; ++u)
+                if (NT - 1 - tid + u * NT < WORDS) mv[u] = *place(NT - 1 - tid + u * NT, slot);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
+        Gr::finish(acc);
+        __syncthreads();                                       // the incoming token is there; the previous pass has been combined
+        if (g == 0) { s_m[wid][2 * t] = m0; s_m[wid][2 * t + 1] = m1; s_l[wid][2 * t] = l0; s_l[wid][2 * t + 1] = l1; }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int ch = Gr::channel(i, g);
+            if (2 * t < nq) *reinterpret_cast<float2*>(&s_acc[wid][2 * t][ch]) = make_float2(acc.a[i][0], acc.a[i][2]);
+            if (2 * t + 1 < nq) *reinterpret_cast<float2*>(&s_acc[wid][2 * t + 1][ch]) = make_float2(acc.a[i][1], acc.a[i][3]);
+        }
+        if (rank == 0)                                         // the incoming token's logits
+            for (int u = wid; u < nq; u += NW) {
+                float a = 0.f;
+#pragma unroll
+                for (int c = 0; c < CPL; ++c)
+                    a = fmaf(__bfloat162float(q1[((size_t)bh * G + g0 + u) * D + lane + 32 * c]), __bfloat162float(s_kv[0][lane + 32 * c]), a);
+                a = warp_sum(a);
+                if (lane == 0) s_new[u] = a;
+            }
+        __syncthreads();
+        if (shared_head && g0 == 0) cluster.barrier_wait();    // every block of the cluster has started: its shared memory is there
+        const int per = nq * D / nsplit, par = (g0 / MQ) & 1;  // output elements each block of the cluster finishes
+        // reference and sum of a query over this block's rows (and the incoming token, in the first block)
+        auto block_sum = [&](int u, float& m, float& tot) {
+            m = rank == 0 ? fmaxf(s_new[u], -FLT_MAX) : -FLT_MAX;
+#pragma unroll
+            for (int w2 = 0; w2 < NW; ++w2) m = fmaxf(m, s_m[w2][u]);
+            tot = rank == 0 ? exp2_fast((s_new[u] - m) * scale2) : 0.f;
+#pragma unroll
+            for (int w2 = 0; w2 < NW; ++w2) tot = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_l[w2][u], tot);   // (a warp without rows: 0)
+        };
+        for (int e = tid; e < nq * D; e += NT) {
+            const int u = e / D, ch = e - u * D;
+            float m, tot;
+            block_sum(u, m, tot);
+            float o = rank == 0 ? exp2_fast((s_new[u] - m) * scale2) * __bfloat162float(s_kv[1][ch]) : 0.f;
+#pragma unroll
+            for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_acc[w2][u][ch], o);
+            if (!shared_head) {
+                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
+                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * scale + logf(tot);
+            } else {                                           // into the shared memory of the block that finishes this element
+                const int own = e / per;
+                *cluster.map_shared_rank(&s_in[par][rank * per + (e - own * per)], own) = o;
+                if (ch < nsplit) *reinterpret_cast<float2*>(cluster.map_shared_rank(&s_ml[par][rank][u][0], ch)) = make_float2(m, tot);
+            }
+        }
+        auto head_sum = [&](int u, float& m, float& tot) {     // over the whole head, once the blocks have met
+            if (!shared_head) { block_sum(u, m, tot); return; }
+            m = -FLT_MAX; tot = 0.f;
+#pragma unroll
+            for (int r2 = 0; r2 < SPLIT; ++r2) if (r2 < nsplit) m = fmaxf(m, s_ml[par][r2][u][0]);
+#pragma unroll
+            for (int r2 = 0; r2 < SPLIT; ++r2) if (r2 < nsplit) tot = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * scale2), s_ml[par][r2][u][1], tot);
+        };
+        if (shared_head) {
+            cluster.sync();                                    // all shares have arrived, and every row has been read
+            for (int e = tid; e < per; e += NT) {
+                const int el = rank * per + e, u = el / D, ch = el - u * D;
+                float m, tot, o = 0.f;
+                head_sum(u, m, tot);
+                for (int r2 = 0; r2 < nsplit; ++r2) o = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * scale2), s_in[par][r2 * per + e], o);
+                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
+                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * scale + logf(tot);
+            }
+        }
+        if constexpr (ACCUM) {
+            // ---- weights of this warp's rows into their scores.  Every block has read the old ones that its decision needs.
+            float fm = 0.f, fi = 0.f;
+            if (lane < nq) { head_sum(lane, fm, fi); fi = 1.f / fi; }
+            for (int e = lane; e < (kept + 31) / 32 * 32; e += 32) {
+                float a = 0.f;
+                for (int u = 0; u < nq; ++u) {
+                    const float m = __shfl_sync(0xffffffffu, fm, u), inv = __shfl_sync(0xffffffffu, fi, u);
+                    if (e < kept) a = fmaf(exp2_fast((wlog[(size_t)e * nq + u] - m) * scale2), inv, a);
+                }
+                if (e >= kept) continue;
+                if (G > MQ) { if (g0 > 0) a += wsum[e]; wsum[e] = a; }
+                const Span sp = rows.span(first + (e >> 4) * step);
+                const int r = e & 15, row = sp.row + r;
+                if (last && r < sp.n && row != masked_ring && row != masked_pool) {
+                    const bool leaves = row == slot && p >= 0; // (its place may already have the incoming token's score)
+                    const float old = leaves ? zp : zc[row];
+                    zc[leaves ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old, a) : a;
+                }
+            }
+            __syncwarp();                                      // (the next pass writes logits where these were)
+            if (rank == 0 && wid == 0)
+                for (int u = 0; u < nq; ++u) {
+                    const float m = __shfl_sync(0xffffffffu, fm, u), inv = __shfl_sync(0xffffffffu, fi, u);
+                    fresh = fmaf(exp2_fast((s_new[u] - m) * scale2), inv, fresh);
+                }
+        }
+    }
+
+    // ---- write-back: only what changed; every read of the old block lies before the barriers above ------------------
+    if (rank != 0) return;
+    if (dst >= 0)
+#pragma unroll
+        for (int u = 0; u < MOVES; ++u)
+            if (NT - 1 - tid + u * NT < WORDS) *place(NT - 1 - tid + u * NT, W + dst) = mv[u];
+    if constexpr (FOUR) {
+        // the incoming row's codes: eight channels a lane, four lanes a group
+        if (wid == NW - 1) {
+            const int e = min(lane, D / 4 - 1), piece = e % (D / 8), grp = piece / 4, tt = piece % 4;
+            const bool values = e >= D / 8;
+            const uint4 u = reinterpret_cast<const uint4*>(s_kv[values])[piece];
+            float f[8], lo, hi;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(word(u, i) << 16); f[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
+            lo = hi = f[0];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+                bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+            }
+            const uint32_t par = group4(lo, hi, bad);
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= code4(f[i], par) << (4 * i);
+            if (lane < D / 4) {
+                unsigned char* codes = blk + (values ? L.off_v : L.off_k) + (size_t)slot * (D / 2);
+                if (values) {
+                    reinterpret_cast<uint16_t*>(codes)[2 * tt * GR + grp] = (uint16_t)w;
+                    reinterpret_cast<uint16_t*>(codes)[(2 * tt + 1) * GR + grp] = (uint16_t)(w >> 16);
+                } else {
+                    reinterpret_cast<uint32_t*>(codes)[tt * GR + grp] = w;
+                }
+                if (tt == 0) reinterpret_cast<uint32_t*>(blk + (values ? L.off_vp : L.off_kp))[(size_t)slot * GR + grp] = par;
+            }
+        }
+    } else {
+        for (int e = tid; e < WORDS; e += NT) *reinterpret_cast<uint4*>(place(e, slot)) = reinterpret_cast<const uint4*>(s_kv)[e];
+    }
+    if (tid == 0) {
+        if (dst >= 0) pidx[dst] = p;
+        if (ACCUM) {
+            zc[slot] = fresh;
+        } else {
+            if (dst >= 0) zc[W + dst] = zp;
+            float znew = rule.bias ? rule.bias[h] : 0.f;
+            if (jsc >= 0) for (int tap = 0; tap < rule.K; ++tap) znew += s_tap[tap];
+            zc[slot] = -INFINITY;                              // the incoming token is not scored yet ...
+            if (jsc >= 0) zc[jsc % W] = znew;                  // ... unless K == 1 (then jsc == n)
+        }
+        meta[0] = n + 1;
+        meta[1] = cnt_new;
+    }
+}
+
+// How many warps share a head: all warps of the launch are resident at once where that is possible, as in decode_mma.cu.  Under accumulated
+// attention a block's logits have to fit beside those of the SM's other blocks.
+template <bool FOUR, bool ACCUM>
+int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1,
+                    void* o1, float* lse1, cudaStream_t st)
+{
+    int n_sm = 0;
+    if (int e = device_sm_count(&n_sm)) return e;
+    const int BH = p.B * p.H, rows = p.W + p.R, warps = warps_per_sm(p.d) * n_sm, most_w = max_warps(p.d);
+    const int spans = (p.W + 15) / 16 + (p.R + 15) / 16;       // at most
+    const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
+    auto most = [&](int all) { return (spans + all - 1) / all * 16; };         // rows of a warp, `all` of which share the head
+    auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };
+    int nw = 1, nsplit = 1;
+    for (int c : {2, 4, 8})
+        if (c <= most_w && ((BH <= n_sm * (warps_per_sm(p.d) / c) && rows / c >= 16) || smem(c / 2, 1) * (warps_per_sm(p.d) / (c / 2)) > 128 * 1024)) nw = c;
+    if (nw == most_w)
+        while (nsplit < MAX_SPLIT && ((BH * nw * nsplit * 2 <= warps && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
+    auto go = [&](auto d, auto w, auto s) {
+        constexpr int D = decltype(d)::value, NW = decltype(w)::value;
+        if constexpr (NW <= max_warps(D)) {
+            auto kern = decode_rows_mma_kernel<D, NW, decltype(s)::value, FOUR, ACCUM>;
+            static PerDeviceOnce once;
+            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); })) return e;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit);
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim.x = nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+            cfg.attrs = attr; cfg.numAttrs = nsplit > 1 ? 2 : 1;
+            return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
+                                                  (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
+                                                  most(nw * nsplit)));
+        }
+        return (int)LTE_ERR_UNSUPPORTED;
+    };
+    auto widths = [&](auto d, auto s) {
+        switch (nw) {
+            case 1: return go(d, std::integral_constant<int, 1>(), s);
+            case 2: return go(d, std::integral_constant<int, 2>(), s);
+            case 4: return go(d, std::integral_constant<int, 4>(), s);
+            default: return go(d, std::integral_constant<int, 8>(), s);
+        }
+    };
+    switch (p.d) {
+        case 32: return widths(std::integral_constant<int, 32>(), std::false_type());
+        case 64:
+            if constexpr (!FOUR) { if (swz) return widths(std::integral_constant<int, 64>(), std::true_type()); }
+            return widths(std::integral_constant<int, 64>(), std::false_type());
+        case 128: return widths(std::integral_constant<int, 128>(), std::false_type());
+    }
+    return LTE_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+}  // namespace lte
