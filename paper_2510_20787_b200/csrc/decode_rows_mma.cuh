@@ -10,14 +10,14 @@
 // blocks have met; then every warp adds its rows' weights, summed over the query heads, to their scores.  One read and one write of 4 bytes a row.
 //
 // Products are mma.sync m16n8k16: logits S^T[16 rows][8 queries] = K q^T, output O^T[16 channels][8 queries] += V^T P^T, N = 8 queries.
-// Rows in 4 bits.  A code c < 16 becomes the bf16 number 1 + c / 16 by a shift and one three-input logic operation on two codes at a time (the
-// code is the top of the mantissa): exact, no conversion.  With value = zero + c step = (zero - 16 step) + 16 step (1 + c / 16):
-//   logits   per group of 32 channels, 16 step (1 + c/16).q + (zero - 16 step) sum(q): the group's product starts from zero, and its two
-//            scalars, which belong to a row, are applied to the products in fp32 (a lane holds rows g and g + 8 of both);
-//   output   P 16 step takes the place of P, per group, and P (zero - 16 step), which is the same for all channels of a group, is summed beside it.
+// Rows in 4 bits.  A code c becomes the bf16 number 16 + c by a shift and one three-input logic operation on two codes at a time (the code is
+// the top of the mantissa): exact, no conversion.  With value = zero + c step = (zero - 16 step) + step (16 + c):
+//   logits   per group of 32 channels, step (16 + c).q + (zero - 16 step) sum(q): the group's product starts from zero, and its two scalars,
+//            which belong to a row, are applied to the products in fp32 (a lane holds rows g and g + 8 of both);
+//   output   P step takes the place of P, per group, and P (zero - 16 step), which is the same for all channels of a group, is summed beside it.
 // The contraction index may be permuted freely: the nibbles i and i + 4 of a key word are neighbours in it, and so are the two rows whose value
 // units a byte permute joins.  The order of the codes in the cache (cache4.cuh) makes these the words that a lane loads.
-// P (times 16 step) is split into two bf16 terms: 16 bits of mantissa.  With one term o would be off by more than its own rounding: the 1 + c/16
+// P (times step) is split into two bf16 terms: 16 bits of mantissa.  With one term o would be off by more than its own rounding: the 16 + c
 // are all positive, so that o is the small difference of sums as large as the rows.
 #pragma once
 #include <cfloat>
@@ -37,16 +37,10 @@ __host__ __device__ constexpr int warps_per_sm(int d) { return d == 128 ? 8 : 16
 __host__ __device__ constexpr int max_warps(int d) { return d == 128 ? 4 : 8; }       // per block
 constexpr int MAX_SPLIT = 8;                                   // blocks per head
 
-struct Span { int row, n; };                                   // up to 16 consecutive rows of the ring or of the pool
+// A head's rows in use: rows 0 .. total - 1 of the block (while the ring fills up the pool is empty), as spans of 16.
 struct Rows {
     const unsigned char *K, *V, *KP, *VP;
-    int n_ring, cnt, W, ring_spans, spans;
-    __device__ __forceinline__ Span span(int i) const
-    {
-        const bool ring = i < ring_spans;
-        const int at = (ring ? i : i - ring_spans) << 4;
-        return {ring ? at : W + at, min(16, (ring ? n_ring : cnt) - at)};
-    }
+    int total;
 };
 
 // What a lane (g, t) = (lane / 4, lane % 4) holds of a span's 16 rows, and the two products with it.  Rows past the end of a span repeat its
@@ -64,33 +58,34 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 #pragma unroll
         for (int j = 0; j < KP; ++j) Q.f[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ void load_k(const Rows& R, const Span& s, int g, int t)
+    // span i; all its rows are there (FULL), or rows past the last one repeat it.  (Row r of a span has the swizzle of r: spans start at multiples of 8.)
+    template <bool FULL> __device__ __forceinline__ void load_k(const Rows& R, int i, int g, int t)
     {
-        const unsigned char* base = R.K + (size_t)s.row * PITCH;
+        const unsigned char* base = R.K + (size_t)i * (16 * PITCH);
+        const int n = R.total - 16 * i;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1), sw = SWZ ? (s.row + r) & 7 : 0;
-            const unsigned char* p = base + r * PITCH;
+        for (int u = 0; u < 2; ++u) {
+            const int r = FULL ? g + 8 * u : min(g + 8 * u, n - 1), sw = SWZ ? r & 7 : 0;
 #pragma unroll
-            for (int j = 0; j < KP; ++j) k[i][j] = *reinterpret_cast<const uint4*>(p + (((t + 4 * j) ^ sw) << 4));
+            for (int j = 0; j < KP; ++j) k[u][j] = *reinterpret_cast<const uint4*>(base + r * PITCH + (((t + 4 * j) ^ sw) << 4));
         }
     }
-    __device__ __forceinline__ void load_v(const Rows& R, const Span& s, int g, int t)
+    template <bool FULL> __device__ __forceinline__ void load_v(const Rows& R, int i, int g, int t)
     {
-        const unsigned char* base = R.V + (size_t)s.row * PITCH;
+        const unsigned char* base = R.V + (size_t)i * (16 * PITCH);
+        const int n = R.total - 16 * i;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int ri = 2 * t + (i & 1) + 8 * (i >> 1), r = s.n == 16 ? ri : min(ri, s.n - 1), sw = SWZ ? (s.row + r) & 7 : 0;
-            const unsigned char* p = base + r * PITCH;
+        for (int u = 0; u < 4; ++u) {
+            const int ru = 2 * t + (u & 1) + 8 * (u >> 1), r = FULL ? ru : min(ru, n - 1), sw = SWZ ? r & 7 : 0;
             if constexpr (D == 32) {
-                const uint2 u = *reinterpret_cast<const uint2*>(p + (g << 3));
-                v[i][0] = u.x; v[i][1] = u.y;
+                const uint2 x = *reinterpret_cast<const uint2*>(base + r * PITCH + (g << 3));
+                v[u][0] = x.x; v[u][1] = x.y;
             } else {
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(p + (((g + 8 * j) ^ sw) << 4));
+                    const uint4 x = *reinterpret_cast<const uint4*>(base + r * PITCH + (((g + 8 * j) ^ sw) << 4));
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) v[i][4 * j + w] = word(u, w);
+                    for (int w = 0; w < 4; ++w) v[u][4 * j + w] = word(x, w);
                 }
             }
         }
@@ -154,11 +149,11 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     static __device__ __forceinline__ int channel(int m, int g) { return D == 32 ? g * 4 + 2 * m : (m >> 2) * 64 + g * 8 + 2 * (m & 3); }
 };
 
-// two codes of a word, at bits 4i and 4i + 16, as the bf16 numbers 1 + c / 16
+// two codes of a word, at bits 4i and 4i + 16, as the bf16 numbers 16 + c
 template <int I> __device__ __forceinline__ uint32_t codes2(uint32_t x)
 {
     const uint32_t y = I == 0 ? x << 3 : x >> (4 * I - 3);
-    return (y & 0x00780078u) | 0x3f803f80u;
+    return (y & 0x00780078u) | 0x41804180u;
 }
 
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
@@ -190,29 +185,30 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3) + 4);
         }
     }
-    __device__ __forceinline__ void load_k(const Rows& R, const Span& s, int g, int t)
+    template <bool FULL> __device__ __forceinline__ void load_k(const Rows& R, int i, int g, int t)
     {
+        const unsigned char *base = R.K + (size_t)i * (8 * D) + t * (4 * GR), *par = R.KP + (size_t)i * (64 * GR);
+        const int n = R.total - 16 * i;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1);
-            get<Words>(k[i], R.K + (size_t)s.row * (D / 2) + r * (D / 2) + t * (4 * GR));
-            get<Words>(kp[i], R.KP + (size_t)s.row * (4 * GR) + r * (4 * GR));
+        for (int u = 0; u < 2; ++u) {
+            const int r = FULL ? g + 8 * u : min(g + 8 * u, n - 1);
+            get<Words>(k[u], base + r * (D / 2));
+            get<Words>(kp[u], par + r * (4 * GR));
         }
     }
-    __device__ __forceinline__ void load_v(const Rows& R, const Span& s, int g, int t)
+    template <bool FULL> __device__ __forceinline__ void load_v(const Rows& R, int i, int g, int t)
     {
+        const unsigned char *base = R.V + (size_t)i * (8 * D) + g * (2 * GR), *par = R.VP + (size_t)i * (64 * GR);
+        const int n = R.total - 16 * i;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int ri = 2 * t + (i & 1) + 8 * (i >> 1), r = s.n == 16 ? ri : min(ri, s.n - 1);
-            const Units u = *reinterpret_cast<const Units*>(R.V + (size_t)s.row * (D / 2) + r * (D / 2) + g * (2 * GR));
-            if constexpr (GR == 1) v[i][0] = u;
-            else memcpy(v[i], &u, sizeof(u));
+        for (int u = 0; u < 4; ++u) {
+            const int ru = 2 * t + (u & 1) + 8 * (u >> 1), r = FULL ? ru : min(ru, n - 1);
+            const Units x = *reinterpret_cast<const Units*>(base + r * (D / 2));
+            if constexpr (GR == 1) v[u][0] = x;
+            else memcpy(v[u], &x, sizeof(x));
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = s.n == 16 ? g + 8 * i : min(g + 8 * i, s.n - 1);
-            get<Words>(vp[i], R.VP + (size_t)s.row * (4 * GR) + r * (4 * GR));
-        }
+        for (int u = 0; u < 2; ++u) get<Words>(vp[u], par + (FULL ? g + 8 * u : min(g + 8 * u, n - 1)) * (4 * GR));
     }
     __device__ __forceinline__ void logits(float (&c)[4], const Query& Q) const
     {
@@ -223,11 +219,11 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             mma16816(p, codes2<2>(k[0][j]), codes2<2>(k[1][j]), codes2<3>(k[0][j]), codes2<3>(k[1][j]), Q.f[j][2], Q.f[j][3]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float s16 = 16.f * par4_step(kp[i][j]), z16 = par4_zero(kp[i][j]) - s16;
+                const float s = par4_step(kp[i][j]), z = fmaf(-16.f, s, par4_zero(kp[i][j]));
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float x = z16 * Q.sum[j][e];
-                    c[2 * i + e] = j == 0 ? fmaf(s16, p[2 * i + e], x) : c[2 * i + e] + fmaf(s16, p[2 * i + e], x);
+                    const float x = fmaf(s, p[2 * i + e], z * Q.sum[j][e]);
+                    c[2 * i + e] = j == 0 ? x : c[2 * i + e] + x;
                 }
             }
         }
@@ -258,8 +254,8 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     {
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
-            const float s0 = 16.f * par4_step(vp[0][j]), s1 = 16.f * par4_step(vp[1][j]);
-            const float z0 = par4_zero(vp[0][j]) - s0, z1 = par4_zero(vp[1][j]) - s1;
+            const float s0 = par4_step(vp[0][j]), s1 = par4_step(vp[1][j]);
+            const float z0 = fmaf(-16.f, s0, par4_zero(vp[0][j])), z1 = fmaf(-16.f, s1, par4_zero(vp[1][j]));
             A.z[j][0] = fmaf(p2, z1, fmaf(p0, z0, A.z[j][0]));
             A.z[j][1] = fmaf(p3, z1, fmaf(p1, z0, A.z[j][1]));
             const float x0 = p0 * s0, x1 = p1 * s0, x2 = p2 * s1, x3 = p3 * s1;
@@ -347,17 +343,16 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
     const int slot = n % W, p = n - W, half = rule.K / 2;
     Rows rows;
     rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
-    rows.W = W; rows.cnt = cnt_old;
-    rows.n_ring = min(n, W);
-    rows.ring_spans = (rows.n_ring + 15) >> 4;
-    rows.spans = rows.ring_spans + ((cnt_old + 15) >> 4);
+    rows.total = n < W ? n : W + cnt_old;
+    const int spans = (rows.total + 15) >> 4, full = rows.total >> 4;
     const int step = NW * nsplit, first = wid * nsplit + rank;
-    auto has = [&](int i) { return i < rows.spans; };
+    auto load_k = [&](Gr& u, int i) { if (i < full) u.template load_k<true>(rows, i, g, t); else u.template load_k<false>(rows, i, g, t); };
+    auto load_v = [&](Gr& u, int i) { if (i < full) u.template load_v<true>(rows, i, g, t); else u.template load_v<false>(rows, i, g, t); };
     Gr buf[NBUF];
     const float zp = p >= 0 ? zc[slot] : 0.f;
 #pragma unroll
     for (int b = 0; b < NBUF; ++b)
-        if (has(first + b * step)) { const Span sp = rows.span(first + b * step); buf[b].load_k(rows, sp, g, t); buf[b].load_v(rows, sp, g, t); }
+        if (first + b * step < spans) { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
     // learned rule: channels lane, lane + 32, .. of the row under a tap, as the cache holds it
     const int jsc = ACCUM ? -1 : n - half;
     auto tap_rows = [&](int tap, float (&kx)[CPL], float (&vx)[CPL]) {
@@ -448,7 +443,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
             Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
 #pragma unroll
             for (int b = 0; b < NBUF; ++b)
-                if (has(first + b * step)) { const Span sp = rows.span(first + b * step); buf[b].load_k(rows, sp, g, t); buf[b].load_v(rows, sp, g, t); }
+                if (first + b * step < spans) { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
         }
         typename Gr::Acc acc;
         Gr::start(acc);
@@ -457,13 +452,12 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
 
         // one span; its registers are refilled with the warp's span NBUF steps ahead as soon as a product has taken them
         auto compute = [&](Gr& u, int i) {
-            const Span cur = rows.span(i), nxt = rows.span(i + NBUF * step);
-            const bool more = has(i + NBUF * step);
+            const int next = i + NBUF * step;
             float c[4];
             u.logits(c, qf);
-            if (more) u.load_k(rows, nxt, g, t);
-            if (cur.n < 16 || (unsigned)(masked_ring - cur.row) < 16u || (unsigned)(masked_pool - cur.row) < 16u) {
-                auto out = [&](int r) { return r >= cur.n || cur.row + r == masked_ring || cur.row + r == masked_pool; };
+            if (next < spans) load_k(u, next);
+            if (i >= full || i == masked_ring >> 4 || i == masked_pool >> 4) {
+                auto out = [&](int r) { const int row = 16 * i + r; return row >= rows.total || row == masked_ring || row == masked_pool; };
                 if (out(g)) c[0] = c[1] = -INFINITY;
                 if (out(g + 8)) c[2] = c[3] = -INFINITY;
                 u.clear(out, g, t);
@@ -494,12 +488,12 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
             const float p2 = exp2_fast((c[2] - m0) * scale2), p3 = exp2_fast((c[3] - m1) * scale2);
             l0 += p0 + p2; l1 += p1 + p3;
             u.output(acc, p0, p1, p2, p3);
-            if (more) u.load_v(rows, nxt, g, t);
+            if (next < spans) load_v(u, next);
         };
-        for (int i = first; has(i); i += NBUF * step) {
+        for (int i = first; i < spans; i += NBUF * step) {
 #pragma unroll
             for (int b = 0; b < NBUF; ++b)
-                if (has(i + b * step)) compute(buf[b], i + b * step);
+                if (i + b * step < spans) compute(buf[b], i + b * step);
         }
         const bool last = g0 + MQ >= G;
         if (rank == 0 && last && dst >= 0)                     // (back by the time the write-back needs them)
@@ -585,9 +579,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
                 }
                 if (e >= kept) continue;
                 if (G > MQ) { if (g0 > 0) a += wsum[e]; wsum[e] = a; }
-                const Span sp = rows.span(first + (e >> 4) * step);
-                const int r = e & 15, row = sp.row + r;
-                if (last && r < sp.n && row != masked_ring && row != masked_pool) {
+                const int row = 16 * (first + (e >> 4) * step) + (e & 15);
+                if (last && row < rows.total && row != masked_ring && row != masked_pool) {
                     const bool leaves = row == slot && p >= 0; // (its place may already have the incoming token's score)
                     const float old = leaves ? zp : zc[row];
                     zc[leaves ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old, a) : a;
@@ -670,7 +663,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R, warps = warps_per_sm(p.d) * n_sm, most_w = max_warps(p.d);
-    const int spans = (p.W + 15) / 16 + (p.R + 15) / 16;       // at most
+    const int spans = (rows + 15) / 16;                        // at most
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
     auto most = [&](int all) { return (spans + all - 1) / all * 16; };         // rows of a warp, `all` of which share the head
     auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };
