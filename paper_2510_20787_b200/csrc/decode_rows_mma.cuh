@@ -27,6 +27,7 @@
 
 #include "decode_rows.cuh"
 #include "row_mma.cuh"
+#include "tc_common.cuh"
 
 namespace lte {
 namespace cg = cooperative_groups;
@@ -146,19 +147,25 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
         }
     }
     static __device__ __forceinline__ void finish(Acc&) {}
+    static __device__ __forceinline__ int rho(int g) { return g; }
     static __device__ __forceinline__ int channel(int m, int g) { return D == 32 ? g * 4 + 2 * m : (m >> 2) * 64 + g * 8 + 2 * (m & 3); }
 };
 
 // two codes of a word, at bits 4i and 4i + 16, as the bf16 numbers 16 + c
-template <int I> __device__ __forceinline__ uint32_t codes2(uint32_t x)
+// (one LOP3: with both constants as immediates the compiler takes two)
+__device__ __forceinline__ uint32_t reg(uint32_t x) { asm("" : "+r"(x)); return x; }
+template <int I> __device__ __forceinline__ uint32_t codes2(uint32_t x, uint32_t mask, uint32_t sixteen)
 {
     const uint32_t y = I == 0 ? x << 3 : x >> (4 * I - 3);
-    return (y & 0x00780078u) | 0x41804180u;
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(y), "r"(mask), "r"(sixteen));     // (y & mask) | sixteen
+    return r;
 }
 
+// Rows in 4 bits: a span stands in shared memory, where the products take their operands from.  M-row r of a product is row rho(r) of the span,
+// rho(2t + b + 8c) = t + 4b + 8c: the value units that the lanes load at once then lie in different banks.
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static constexpr int GR = D / kGroup4, MT = D / 16;
-    uint32_t k[2][GR], kp[2][GR], v[4][(GR + 1) / 2], vp[2][GR];   // of rows g, g + 8 (values: units g of rows 2t, 2t + 1, 2t + 8, 2t + 9)
     struct Query { uint32_t f[GR][4]; float sum[GR][2]; };     // of query g; sums of queries 2t, 2t + 1 over a group's channels
     struct Acc { float a[MT][4], z[GR][2]; };
     template <typename U> static __device__ __forceinline__ void get(uint32_t (&x)[GR], const unsigned char* p)
@@ -168,6 +175,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     }
     using Words = std::conditional_t<GR == 1, uint32_t, std::conditional_t<GR == 2, uint2, uint4>>;
     using Units = std::conditional_t<GR == 1, uint16_t, std::conditional_t<GR == 2, uint32_t, uint2>>;
+    static __device__ __forceinline__ int rho(int g) { return (g >> 1) + 4 * (g & 1); }     // (g < 8)
     static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
     {
         const int lane = 4 * g + t;
@@ -185,38 +193,21 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3) + 4);
         }
     }
-    template <bool FULL> __device__ __forceinline__ void load_k(const Rows& R, int i, int g, int t)
+    // keys, parameters: of this span's first row
+    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* keys, const unsigned char* pars, int g, int t)
     {
-        const unsigned char *base = R.K + (size_t)i * (8 * D) + t * (4 * GR), *par = R.KP + (size_t)i * (64 * GR);
-        const int n = R.total - 16 * i;
+        const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
+        uint32_t k[2][GR], kp[2][GR];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int r = FULL ? g + 8 * u : min(g + 8 * u, n - 1);
-            get<Words>(k[u], base + r * (D / 2));
-            get<Words>(kp[u], par + r * (4 * GR));
+            get<Words>(k[u], keys + (rho(g) + 8 * u) * (D / 2) + t * (4 * GR));
+            get<Words>(kp[u], pars + (rho(g) + 8 * u) * (4 * GR));
         }
-    }
-    template <bool FULL> __device__ __forceinline__ void load_v(const Rows& R, int i, int g, int t)
-    {
-        const unsigned char *base = R.V + (size_t)i * (8 * D) + g * (2 * GR), *par = R.VP + (size_t)i * (64 * GR);
-        const int n = R.total - 16 * i;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int ru = 2 * t + (u & 1) + 8 * (u >> 1), r = FULL ? ru : min(ru, n - 1);
-            const Units x = *reinterpret_cast<const Units*>(base + r * (D / 2));
-            if constexpr (GR == 1) v[u][0] = x;
-            else memcpy(v[u], &x, sizeof(x));
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) get<Words>(vp[u], par + (FULL ? g + 8 * u : min(g + 8 * u, n - 1)) * (4 * GR));
-    }
-    __device__ __forceinline__ void logits(float (&c)[4], const Query& Q) const
-    {
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
             float p[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816(p, codes2<0>(k[0][j]), codes2<0>(k[1][j]), codes2<1>(k[0][j]), codes2<1>(k[1][j]), Q.f[j][0], Q.f[j][1]);
-            mma16816(p, codes2<2>(k[0][j]), codes2<2>(k[1][j]), codes2<3>(k[0][j]), codes2<3>(k[1][j]), Q.f[j][2], Q.f[j][3]);
+            mma16816(p, codes2<0>(k[0][j], M, S), codes2<0>(k[1][j], M, S), codes2<1>(k[0][j], M, S), codes2<1>(k[1][j], M, S), Q.f[j][0], Q.f[j][1]);
+            mma16816(p, codes2<2>(k[0][j], M, S), codes2<2>(k[1][j], M, S), codes2<3>(k[0][j], M, S), codes2<3>(k[1][j], M, S), Q.f[j][2], Q.f[j][3]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float s = par4_step(kp[i][j]), z = fmaf(-16.f, s, par4_zero(kp[i][j]));
@@ -227,14 +218,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
                 }
             }
         }
-    }
-    template <typename F> __device__ __forceinline__ void clear(F&& out, int g, int)
-    {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (out(g + 8 * i))
-#pragma unroll
-                for (int j = 0; j < GR; ++j) vp[i][j] = 0u;
     }
     static __device__ __forceinline__ void start(Acc& A)
     {
@@ -250,28 +233,47 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
     }
-    __device__ __forceinline__ void output(Acc& A, float p0, float p1, float p2, float p3) const
+    // gone: bit 0, 1: the rows of M-rows g, g + 8 do not count
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* values, const unsigned char* pars, unsigned gone, int g, int t)
     {
+        const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
+        uint32_t v[4][(GR + 1) / 2], vp[2][GR];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const Units x = *reinterpret_cast<const Units*>(values + (t + 4 * u) * (D / 2) + g * (2 * GR));   // M-rows 2t + (u & 1) + 8 (u / 2)
+            if constexpr (GR == 1) v[u][0] = x;
+            else memcpy(v[u], &x, sizeof(x));
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) get<Words>(vp[u], pars + (rho(g) + 8 * u) * (4 * GR));
+        if (gone & 1u)
+#pragma unroll
+            for (int j = 0; j < GR; ++j) vp[0][j] = 0u;
+        if (gone & 2u)
+#pragma unroll
+            for (int j = 0; j < GR; ++j) vp[1][j] = 0u;
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
             const float s0 = par4_step(vp[0][j]), s1 = par4_step(vp[1][j]);
             const float z0 = fmaf(-16.f, s0, par4_zero(vp[0][j])), z1 = fmaf(-16.f, s1, par4_zero(vp[1][j]));
-            A.z[j][0] = fmaf(p2, z1, fmaf(p0, z0, A.z[j][0]));
-            A.z[j][1] = fmaf(p3, z1, fmaf(p1, z0, A.z[j][1]));
-            const float x0 = p0 * s0, x1 = p1 * s0, x2 = p2 * s1, x3 = p3 * s1;
+            A.z[j][0] = fmaf(p[2], z1, fmaf(p[0], z0, A.z[j][0]));
+            A.z[j][1] = fmaf(p[3], z1, fmaf(p[1], z0, A.z[j][1]));
+            const float x0 = p[0] * s0, x1 = p[1] * s0, x2 = p[2] * s1, x3 = p[3] * s1;
             const uint32_t hi0 = pack_bf16(x0, x1), hi1 = pack_bf16(x2, x3);
             const uint32_t lo0 = pack_bf16(x0 - __uint_as_float(hi0 << 16), x1 - __uint_as_float(hi0 & 0xffff0000u));
             const uint32_t lo1 = pack_bf16(x2 - __uint_as_float(hi1 << 16), x3 - __uint_as_float(hi1 & 0xffff0000u));
             const uint32_t h0 = movmatrix_trans(hi0), h1 = movmatrix_trans(hi1), e0 = movmatrix_trans(lo0), e1 = movmatrix_trans(lo1);
-            const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410);   // four codes of row 2t, of row 2t + 1
+            const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410);   // four codes of M-row 2t, of M-row 2t + 1
             const uint32_t w = __byte_perm(v[2][j / 2], v[3][j / 2], j & 1 ? 0x7632 : 0x5410);
-            mma16816(A.a[2 * j], codes2<0>(u), codes2<1>(u), codes2<0>(w), codes2<1>(w), h0, h1);
-            mma16816(A.a[2 * j], codes2<0>(u), codes2<1>(u), codes2<0>(w), codes2<1>(w), e0, e1);
-            mma16816(A.a[2 * j + 1], codes2<2>(u), codes2<3>(u), codes2<2>(w), codes2<3>(w), h0, h1);
-            mma16816(A.a[2 * j + 1], codes2<2>(u), codes2<3>(u), codes2<2>(w), codes2<3>(w), e0, e1);
+            const uint32_t u0 = codes2<0>(u, M, S), u1 = codes2<1>(u, M, S), u2 = codes2<2>(u, M, S), u3 = codes2<3>(u, M, S);
+            const uint32_t w0 = codes2<0>(w, M, S), w1 = codes2<1>(w, M, S), w2 = codes2<2>(w, M, S), w3 = codes2<3>(w, M, S);
+            mma16816(A.a[2 * j], u0, u1, w0, w1, h0, h1);
+            mma16816(A.a[2 * j + 1], u2, u3, w2, w3, h0, h1);
+            mma16816(A.a[2 * j], u0, u1, w0, w1, e0, e1);
+            mma16816(A.a[2 * j + 1], u2, u3, w2, w3, e0, e1);
         }
     }
-    // the groups' constant parts, summed over the lanes of a query, into the outputs (of one lane's rows each: lanes g = 0)
+    // the groups' constant parts, summed over the lanes of a query, into the outputs
     static __device__ __forceinline__ void finish(Acc& A)
     {
 #pragma unroll
@@ -287,6 +289,20 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
 };
 
+// Stages of shared memory through which a warp's units of a cache in 4 bits pass: bulk copies that the warp's lane 0 starts, a barrier per stage.
+// (In registers, as bf16 rows are, enough units in flight and the products' operands do not fit 128 registers, and every load costs
+// its address arithmetic in every lane.)
+template <int D> struct Stage4 {
+    static constexpr int UR = 32, STAGES = 3, K = 0, V = UR * D / 2, KP = 2 * V, VP = KP + UR * D / 8, BYTES = VP + UR * D / 8;
+};
+
+__device__ StatusWord g_rows_status = LTE_STATUS_INIT;
+
+__device__ __forceinline__ void bulk_copy(uint32_t to, const unsigned char* from, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
 template <int D, int NW, bool SWZ, bool FOUR, bool ACCUM>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
@@ -295,9 +311,15 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
 {
     using Gr = Group<D, SWZ, FOUR>;
     constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
-    constexpr int NBUF = FOUR ? 3 : 2;                         // spans in flight per warp
+    // A warp takes UNIT spans at a time, NBUF times as many in flight.  (4 bits: two at a time, so that instructions of one fill the other's
+    // latencies; bf16 waits for memory.)
+    constexpr int UNIT = FOUR ? 2 : 1, UR = 16 * UNIT;
+    using St = Stage4<D>;
+    constexpr int NBUF = FOUR ? St::STAGES : 2;
     constexpr int SPLIT = NW == max_warps(D) ? MAX_SPLIT : 1;  // (only the largest blocks come in clusters)
-    extern __shared__ __align__(16) float s_log[];             // [NW][most][nq], behind them [NW][most] sums over passes
+    extern __shared__ __align__(128) unsigned char s_dyn[];    // 4 bits: the warps' stages; [NW][most][nq] logits, behind them [NW][most] sums over passes
+    float* const s_log = reinterpret_cast<float*>(s_dyn + (FOUR ? NW * St::STAGES * St::BYTES : 0));
+    __shared__ __align__(8) uint64_t s_bar[FOUR ? NW * St::STAGES : 1];
     __shared__ __align__(16) float s_acc[NW][MQ][PITCH];
     __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
     __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
@@ -317,9 +339,51 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
     const bool shared_head = SPLIT > 1 && nsplit > 1;          // (uniform in the cluster)
     if (shared_head) cluster.barrier_arrive();                 // (awaited before the first store into another block's shared memory)
     pdl_launch_dependents();
+    if constexpr (FOUR) {
+        if (lane == 0) {
+            for (int i = 0; i < St::STAGES; ++i) tc::mbar_init(tc::smem_u32(&s_bar[wid * St::STAGES + i]), 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    }
     pdl_wait();
 
-    // Everything whose address is known is asked for at once, then everything that needs the counters.
+    // Everything whose address is known is asked for at once: the rows that a warp begins with too, whether or not they turn out to be in use.
+    Rows rows;
+    rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
+    rows.total = W + R;
+    const int step = NW * nsplit, first = wid * nsplit + rank;
+    // bf16: registers
+    Gr buf[FOUR ? 1 : NBUF];
+    auto load_k = [&](Gr& u, int i) { if constexpr (!FOUR) { if (UR * (i + 1) <= rows.total) u.template load_k<true>(rows, i, g, t); else u.template load_k<false>(rows, i, g, t); } };
+    auto load_v = [&](Gr& u, int i) { if constexpr (!FOUR) { if (UR * (i + 1) <= rows.total) u.template load_v<true>(rows, i, g, t); else u.template load_v<false>(rows, i, g, t); } };
+    // 4 bits: unit number j of this warp goes through stage j % STAGES; `asked` and `taken` count over all passes
+    unsigned char* const stage = s_dyn + wid * (St::STAGES * St::BYTES);
+    const uint32_t bar = tc::smem_u32(&s_bar[FOUR ? wid * St::STAGES : 0]);
+    int asked = 0, taken = 0;
+    auto ask = [&](int i) {
+        if constexpr (FOUR) {
+            if (lane == 0) {
+                const uint32_t nr = min(UR, rows.total - UR * i), row = nr * (D / 2), par = (nr * (4 * GR) + 15) & ~15u;   // (a part's size in the cache is a multiple of 16)
+                const uint32_t b = bar + 8 * (asked % St::STAGES), to = tc::smem_u32(stage + (asked % St::STAGES) * St::BYTES);
+                tc::mbar_expect_tx(b, 2 * (row + par));
+                bulk_copy(to + St::K, rows.K + (size_t)i * (UR * D / 2), row, b);
+                bulk_copy(to + St::KP, rows.KP + (size_t)i * (UR * 4 * GR), par, b);
+                bulk_copy(to + St::V, rows.V + (size_t)i * (UR * D / 2), row, b);
+                bulk_copy(to + St::VP, rows.VP + (size_t)i * (UR * 4 * GR), par, b);
+            }
+            ++asked;
+        }
+    };
+    auto begin = [&](int units_there) {                        // the first units of a pass
+#pragma unroll
+        for (int b = 0; b < NBUF; ++b)
+            if (first + b * step < units_there) {
+                if constexpr (FOUR) ask(first + b * step);
+                else { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
+            }
+    };
+    begin((rows.total + UR - 1) / UR);
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
     typename Gr::Query qf;
     Gr::load_q(qf, q1 + (size_t)bh * G * D, g < G, g, t);
@@ -341,18 +405,9 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         wv[c] = taps ? rule.w[((size_t)h * rule.K + wid) * 2 * D + D + lane + 32 * c] : 0.f;
     }
     const int slot = n % W, p = n - W, half = rule.K / 2;
-    Rows rows;
-    rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
     rows.total = n < W ? n : W + cnt_old;
-    const int spans = (rows.total + 15) >> 4, full = rows.total >> 4;
-    const int step = NW * nsplit, first = wid * nsplit + rank;
-    auto load_k = [&](Gr& u, int i) { if (i < full) u.template load_k<true>(rows, i, g, t); else u.template load_k<false>(rows, i, g, t); };
-    auto load_v = [&](Gr& u, int i) { if (i < full) u.template load_v<true>(rows, i, g, t); else u.template load_v<false>(rows, i, g, t); };
-    Gr buf[NBUF];
+    const int units = (rows.total + UR - 1) / UR, full = rows.total / UR;
     const float zp = p >= 0 ? zc[slot] : 0.f;
-#pragma unroll
-    for (int b = 0; b < NBUF; ++b)
-        if (first + b * step < spans) { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
     // learned rule: channels lane, lane + 32, .. of the row under a tap, as the cache holds it
     const int jsc = ACCUM ? -1 : n - half;
     auto tap_rows = [&](int tap, float (&kx)[CPL], float (&vx)[CPL]) {
@@ -441,36 +496,50 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         const int nq = min(MQ, G - g0);
         if (g0 > 0) {                                          // further query heads read the rows again
             Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
-#pragma unroll
-            for (int b = 0; b < NBUF; ++b)
-                if (first + b * step < spans) { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
+            begin(units);
         }
         typename Gr::Acc acc;
         Gr::start(acc);
         float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
         int kept = 0;                                          // rows whose logits this warp has kept
 
-        // one span; its registers are refilled with the warp's span NBUF steps ahead as soon as a product has taken them
-        auto compute = [&](Gr& u, int i) {
+        // one unit; its registers (or its stage) are refilled with the warp's unit NBUF steps ahead as soon as the products have taken them
+        auto compute = [&](int b, int i) {
             const int next = i + NBUF * step;
-            float c[4];
-            u.logits(c, qf);
-            if (next < spans) load_k(u, next);
-            if (i >= full || i == masked_ring >> 4 || i == masked_pool >> 4) {
-                auto out = [&](int r) { const int row = 16 * i + r; return row >= rows.total || row == masked_ring || row == masked_pool; };
-                if (out(g)) c[0] = c[1] = -INFINITY;
-                if (out(g + 8)) c[2] = c[3] = -INFINITY;
-                u.clear(out, g, t);
+            float c[UNIT][4], p[UNIT][4];
+            const unsigned char* at4 = stage + (taken % St::STAGES) * St::BYTES;
+            if constexpr (FOUR) {
+                tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, 1, &g_rows_status);
+#pragma unroll
+                for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, at4 + St::K + x * (8 * D), at4 + St::KP + x * (64 * GR), g, t);
+            } else {
+                buf[b].logits(c[0], qf);
+                if (next < units) load_k(buf[b], next);
+            }
+            unsigned gone[UNIT] = {};
+            if (i >= full || i == masked_ring / UR || i == masked_pool / UR) {
+#pragma unroll
+                for (int x = 0; x < UNIT; ++x) {
+                    auto out = [&](int r) { const int row = UR * i + 16 * x + r; return row >= rows.total || row == masked_ring || row == masked_pool; };
+                    if (out(Gr::rho(g))) { c[x][0] = c[x][1] = -INFINITY; gone[x] |= 1u; }
+                    if (out(Gr::rho(g) + 8)) { c[x][2] = c[x][3] = -INFINITY; gone[x] |= 2u; }
+                    if constexpr (!FOUR) buf[b].clear(out, g, t);
+                }
             }
             if constexpr (ACCUM) {                             // raw logits [row][query]
-                float* at = wlog + (size_t)(kept + g) * nq + 2 * t;
-                if (2 * t < nq) { at[0] = c[0]; at[8 * nq] = c[2]; }
-                if (2 * t + 1 < nq) { at[1] = c[1]; at[8 * nq + 1] = c[3]; }
-                kept += 16;
+                float* at = wlog + (size_t)(kept + Gr::rho(g)) * nq + 2 * t;
+#pragma unroll
+                for (int x = 0; x < UNIT; ++x) {
+                    if (2 * t < nq) { at[16 * x * nq] = c[x][0]; at[(16 * x + 8) * nq] = c[x][2]; }
+                    if (2 * t + 1 < nq) { at[16 * x * nq + 1] = c[x][1]; at[(16 * x + 8) * nq + 1] = c[x][3]; }
+                }
+                kept += UR;
             }
             // The reference m follows the maximum only when that has grown by 2^8 (weights stay below 2^8, in fp32): a vote per
-            // span instead of a reduction over its rows.
-            const float x0 = fmaxf(c[0], c[2]), x1 = fmaxf(c[1], c[3]);
+            // unit instead of a reduction over its rows.
+            float x0 = fmaxf(c[0][0], c[0][2]), x1 = fmaxf(c[0][1], c[0][3]);
+#pragma unroll
+            for (int x = 1; x < UNIT; ++x) { x0 = fmaxf(x0, fmaxf(c[x][0], c[x][2])); x1 = fmaxf(x1, fmaxf(c[x][1], c[x][3])); }
             if (__any_sync(0xffffffffu, x0 > m0 + jump || x1 > m1 + jump)) {
                 float y0 = x0, y1 = x1;
 #pragma unroll
@@ -484,22 +553,53 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
                 l0 *= f0; l1 *= f1;
                 Gr::rescale(acc, f0, f1);
             }
-            const float p0 = exp2_fast((c[0] - m0) * scale2), p1 = exp2_fast((c[1] - m1) * scale2);
-            const float p2 = exp2_fast((c[2] - m0) * scale2), p3 = exp2_fast((c[3] - m1) * scale2);
-            l0 += p0 + p2; l1 += p1 + p3;
-            u.output(acc, p0, p1, p2, p3);
-            if (next < spans) load_v(u, next);
-        };
-        for (int i = first; i < spans; i += NBUF * step) {
 #pragma unroll
-            for (int b = 0; b < NBUF; ++b)
-                if (i + b * step < spans) compute(buf[b], i + b * step);
+            for (int x = 0; x < UNIT; ++x) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast((c[x][e] - (e & 1 ? m1 : m0)) * scale2);
+                l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3];
+            }
+            if constexpr (FOUR) {
+#pragma unroll
+                for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], at4 + St::V + x * (8 * D), at4 + St::VP + x * (64 * GR), gone[x], g, t);
+                ++taken;
+                __syncwarp();                                  // every lane has read the stage
+                if (next < units) ask(next);
+            } else {
+                buf[b].output(acc, p[0][0], p[0][1], p[0][2], p[0][3]);
+                if (next < units) load_v(buf[b], next);
+            }
+        };
+        if constexpr (FOUR) {
+#pragma unroll 1
+            for (int i = first; i < units; i += step) compute(0, i);
+            for (; taken < asked; ++taken)                     // units asked for before it was known how many rows are in use
+                tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, 2, &g_rows_status);
+        } else {
+            for (int i = first; i < units; i += NBUF * step) {
+#pragma unroll
+                for (int b = 0; b < NBUF; ++b)
+                    if (i + b * step < units) compute(b, i + b * step);
+            }
         }
         const bool last = g0 + MQ >= G;
         if (rank == 0 && last && dst >= 0)                     // (back by the time the write-back needs them)
 #pragma unroll
             for (int u = 0; u < MOVES; ++u)
                 if (NT - 1 - tid + u * NT < WORDS) mv[u] = *place(NT - 1 - tid + u * NT, slot);
+        // Scores of this warp's rows: asked for before the warps meet, a batch at a time.  Row e of a warp is row e % UR of its unit e / UR.
+        auto row_of = [&](int e) { return UR * (first + e / UR * step) + e % UR; };
+        auto counts = [&](int row) { return row < rows.total && row != masked_ring && row != masked_pool; };
+        constexpr int BATCH = 8;
+        float old[BATCH];
+        auto load_old = [&](int e0) {
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int e = e0 + 32 * b, row = row_of(e);
+                old[b] = e < kept && counts(row) ? row == slot && p >= 0 ? zp : zc[row] : 0.f;   // (the popped row's place may already have been written)
+            }
+        };
+        if (ACCUM && last) load_old(lane);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
         Gr::finish(acc);
@@ -569,29 +669,29 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         }
         if constexpr (ACCUM) {
             // ---- weights of this warp's rows into their scores.  Every block has read the old ones that its decision needs.
-            float fm = 0.f, fi = 0.f;
+            float fm = 0.f, fi = 0.f, ms[MQ], is[MQ];
             if (lane < nq) { head_sum(lane, fm, fi); fi = 1.f / fi; }
-            for (int e = lane; e < (kept + 31) / 32 * 32; e += 32) {
-                float a = 0.f;
-                for (int u = 0; u < nq; ++u) {
-                    const float m = __shfl_sync(0xffffffffu, fm, u), inv = __shfl_sync(0xffffffffu, fi, u);
-                    if (e < kept) a = fmaf(exp2_fast((wlog[(size_t)e * nq + u] - m) * scale2), inv, a);
-                }
-                if (e >= kept) continue;
-                if (G > MQ) { if (g0 > 0) a += wsum[e]; wsum[e] = a; }
-                const int row = 16 * (first + (e >> 4) * step) + (e & 15);
-                if (last && row < rows.total && row != masked_ring && row != masked_pool) {
-                    const bool leaves = row == slot && p >= 0; // (its place may already have the incoming token's score)
-                    const float old = leaves ? zp : zc[row];
-                    zc[leaves ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old, a) : a;
+#pragma unroll
+            for (int u = 0; u < MQ; ++u) { ms[u] = __shfl_sync(0xffffffffu, fm, u); is[u] = __shfl_sync(0xffffffffu, fi, u); }
+            for (int e0 = lane; e0 < kept; e0 += 32 * BATCH) {
+                if (last && e0 >= 32 * BATCH) load_old(e0);
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b) {
+                    const int e = e0 + 32 * b, row = row_of(e);
+                    if (e >= kept) break;
+                    float a = 0.f;
+#pragma unroll
+                    for (int u = 0; u < MQ; ++u)
+                        if (u < nq) a = fmaf(exp2_fast((wlog[(size_t)e * nq + u] - ms[u]) * scale2), is[u], a);
+                    if (G > MQ) { if (g0 > 0) a += wsum[e]; wsum[e] = a; }
+                    if (last && counts(row)) zc[row == slot && p >= 0 ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old[b], a) : a;
                 }
             }
             __syncwarp();                                      // (the next pass writes logits where these were)
             if (rank == 0 && wid == 0)
-                for (int u = 0; u < nq; ++u) {
-                    const float m = __shfl_sync(0xffffffffu, fm, u), inv = __shfl_sync(0xffffffffu, fi, u);
-                    fresh = fmaf(exp2_fast((s_new[u] - m) * scale2), inv, fresh);
-                }
+#pragma unroll
+                for (int u = 0; u < MQ; ++u)
+                    if (u < nq) fresh = fmaf(exp2_fast((s_new[u] - ms[u]) * scale2), is[u], fresh);
         }
     }
 
@@ -663,10 +763,10 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R, warps = warps_per_sm(p.d) * n_sm, most_w = max_warps(p.d);
-    const int spans = (rows + 15) / 16;                        // at most
+    constexpr int UR = FOUR ? 32 : 16;                         // rows that a warp takes at a time
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
-    auto most = [&](int all) { return (spans + all - 1) / all * 16; };         // rows of a warp, `all` of which share the head
-    auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };
+    auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
+    auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };   // of logits
     int nw = 1, nsplit = 1;
     for (int c : {2, 4, 8})
         if (c <= most_w && ((BH <= n_sm * (warps_per_sm(p.d) / c) && rows / c >= 16) || smem(c / 2, 1) * (warps_per_sm(p.d) / (c / 2)) > 128 * 1024)) nw = c;
@@ -677,9 +777,9 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         if constexpr (NW <= max_warps(D)) {
             auto kern = decode_rows_mma_kernel<D, NW, decltype(s)::value, FOUR, ACCUM>;
             static PerDeviceOnce once;
-            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); })) return e;
+            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024); })) return e;
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit);
+            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit) + (FOUR ? NW * Stage4<D>::STAGES * Stage4<D>::BYTES : 0);
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
             attr[0].val.programmaticStreamSerializationAllowed = 1;
