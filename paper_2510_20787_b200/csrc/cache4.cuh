@@ -61,12 +61,15 @@ __device__ __forceinline__ uint32_t group4(float lo, float hi, bool bad)
     if (bad || (step & 0x7f80u) == 0x7f80u || (zero & 0x7f80u) == 0x7f80u) return 0x7fc07fc0u;
     return step | (zero << 16);
 }
-// clamp(rint((x - zero) / step), 0, 15) in fp32 arithmetic; 0 where step is 0 or the group NaN
+// clamp(rint((x - zero) / step), 0, 15) in fp32 arithmetic; 0 where step is 0 or the group NaN.  The quotient is taken by the reciprocal, which is
+// off by a few units in the last place: only within 2^-10 of the middle between two codes can that decide, and there it is divided.
 __device__ __forceinline__ uint32_t code4(float x, uint32_t par)
 {
-    const float step = par4_step(par);
+    const float step = par4_step(par), r = x - par4_zero(par);
     if (!(step > 0.f)) return 0u;
-    return (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - par4_zero(par), step)), 0.f), 15.f);
+    float q = r * __frcp_rn(step), c = rintf(q);
+    if (!(fabsf(q - c) < 0.5f - 0x1p-10f)) c = rintf(__fdiv_rn(r, step));    // (so do a quotient and a reciprocal out of range)
+    return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
 }
 
 // A group of the row in `x` (one channel per lane) into the 4-bit cache, by a whole warp.

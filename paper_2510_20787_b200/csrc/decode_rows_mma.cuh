@@ -34,67 +34,51 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int MQ = 8;                                          // query heads per pass
-__host__ __device__ constexpr int warps_per_sm(int d) { return d == 128 ? 8 : 16; }   // resident warps the registers are budgeted for
+// resident warps the registers (and the stages in shared memory) are budgeted for
+__host__ __device__ constexpr int warps_per_sm(int d, bool four) { return d == 128 ? 8 : 16; }
 __host__ __device__ constexpr int max_warps(int d) { return d == 128 ? 4 : 8; }       // per block
 constexpr int MAX_SPLIT = 8;                                   // blocks per head
 
-// A head's rows in use: rows 0 .. total - 1 of the block (while the ring fills up the pool is empty), as spans of 16.
+// A head's rows in use are rows 0 .. total - 1 of its block (while the ring fills up the pool is empty).  A warp takes units of UR of them, 16 to
+// a product, which pass through STAGES of its own in shared memory: bulk copies that its lane 0 starts, a barrier per stage.  (With the units in
+// registers, enough of them in flight and the products' operands did not fit 128 registers, and every load cost its address arithmetic in
+// every lane: 256 heads x 1,280 rows in 4 bits 23.7 us, through shared memory 18.5.)
 struct Rows {
     const unsigned char *K, *V, *KP, *VP;
     int total;
 };
+template <int D, bool FOUR> struct Stage {
+    static constexpr int UR = FOUR ? 32 : 16, STAGES = FOUR ? 3 : 2;
+    static constexpr int ROW = FOUR ? D / 2 : 2 * D, PAR = FOUR ? D / 8 : 0;   // bytes of a row's keys, of its key parameters
+    static constexpr int K = 0, V = UR * ROW, KP = 2 * V, VP = KP + UR * PAR, BYTES = VP + UR * PAR;
+    static constexpr int ACC = MQ * (D + 8) * 4;               // a warp's outputs stand where its stages were
+    static_assert(ACC <= STAGES * BYTES, "");
+};
 
-// What a lane (g, t) = (lane / 4, lane % 4) holds of a span's 16 rows, and the two products with it.  Rows past the end of a span repeat its
-// last row; they and the rows that the step leaves out have weight zero, and what they hold is cleared (zero times an infinite value is NaN).
+// The two products with a span of 16 rows that stands in shared memory, lane (g, t) = (lane / 4, lane % 4).  Rows past the last one and those that the
+// step leaves out have weight zero, and what they hold is cleared (zero times an infinite value is NaN).
 template <int D, bool SWZ, bool FOUR> struct Group;
 
 template <int D, bool SWZ> struct Group<D, SWZ, false> {
-    static constexpr int KP = D / 32, VB = D / 16, PITCH = D * 2, MT = D / 16, GR = 0;
-    uint4 k[2][KP];                                            // pieces t, t + 4, .. of rows g, g + 8
-    uint32_t v[4][VB];                                         // pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9
+    static constexpr int KP = D / 32, VB = D / 16, PITCH = D * 2, MT = D / 16;
     struct Query { uint4 f[KP]; };                             // pieces t, t + 4, .. of query g
     struct Acc { float a[MT][4]; };
+    static __device__ __forceinline__ int rho(int g) { return g; }
     static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
     {
 #pragma unroll
         for (int j = 0; j < KP; ++j) Q.f[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
     }
-    // span i; all its rows are there (FULL), or rows past the last one repeat it.  (Row r of a span has the swizzle of r: spans start at multiples of 8.)
-    template <bool FULL> __device__ __forceinline__ void load_k(const Rows& R, int i, int g, int t)
-    {
-        const unsigned char* base = R.K + (size_t)i * (16 * PITCH);
-        const int n = R.total - 16 * i;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int r = FULL ? g + 8 * u : min(g + 8 * u, n - 1), sw = SWZ ? r & 7 : 0;
-#pragma unroll
-            for (int j = 0; j < KP; ++j) k[u][j] = *reinterpret_cast<const uint4*>(base + r * PITCH + (((t + 4 * j) ^ sw) << 4));
-        }
-    }
-    template <bool FULL> __device__ __forceinline__ void load_v(const Rows& R, int i, int g, int t)
-    {
-        const unsigned char* base = R.V + (size_t)i * (16 * PITCH);
-        const int n = R.total - 16 * i;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int ru = 2 * t + (u & 1) + 8 * (u >> 1), r = FULL ? ru : min(ru, n - 1), sw = SWZ ? r & 7 : 0;
-            if constexpr (D == 32) {
-                const uint2 x = *reinterpret_cast<const uint2*>(base + r * PITCH + (g << 3));
-                v[u][0] = x.x; v[u][1] = x.y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < D / 64; ++j) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(base + r * PITCH + (((g + 8 * j) ^ sw) << 4));
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v[u][4 * j + w] = word(x, w);
-                }
-            }
-        }
-    }
     // c: rows g (0, 1) and g + 8 (2, 3), queries 2t and 2t + 1.  A product rounds its running sum towards zero, so every one starts from zero
-    // and the parts are added to the nearest (see decode_mma.cu).
-    __device__ __forceinline__ void logits(float (&c)[4], const Query& Q) const
+    // and the parts are added to the nearest (see decode_mma.cu).  Lane (g, t) takes pieces t, t + 4, .. of rows g and g + 8.
+    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* st, int span, int g, int t)
     {
+        uint4 k[2][KP];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < KP; ++j)
+                k[u][j] = *reinterpret_cast<const uint4*>(st + Stage<D, false>::K + (16 * span + g + 8 * u) * PITCH + (((t + 4 * j) ^ (SWZ ? g & 7 : 0)) << 4));
         constexpr int NS = D == 128 ? 2 * KP : 1;
         float cs[NS][4];
 #pragma unroll
@@ -114,14 +98,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 #pragma unroll
         for (int e = 0; e < 4; ++e) c[e] = cs[0][e];
     }
-    template <typename F> __device__ __forceinline__ void clear(F&& out, int, int t)         // rows of the span that out(row) names
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (out(2 * t + (i & 1) + 8 * (i >> 1)))
-#pragma unroll
-                for (int j = 0; j < VB; ++j) v[i][j] = 0u;
-    }
     static __device__ __forceinline__ void start(Acc& A)
     {
 #pragma unroll
@@ -132,11 +108,35 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 #pragma unroll
         for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
     }
-    __device__ __forceinline__ void output(Acc& A, float p0, float p1, float p2, float p3) const
+    // gone: bit r: row r of the span does not count.  Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* st, int span, unsigned gone, int g, int t)
     {
-        const uint32_t hi0 = pack_bf16(p0, p1), hi1 = pack_bf16(p2, p3);
-        const uint32_t lo0 = pack_bf16(p0 - __uint_as_float(hi0 << 16), p1 - __uint_as_float(hi0 & 0xffff0000u));
-        const uint32_t lo1 = pack_bf16(p2 - __uint_as_float(hi1 << 16), p3 - __uint_as_float(hi1 & 0xffff0000u));
+        uint32_t v[4][VB];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int r = 2 * t + (u & 1) + 8 * (u >> 1);
+            const unsigned char* base = st + Stage<D, false>::V + (16 * span + r) * PITCH;
+            if constexpr (D == 32) {
+                const uint2 x = *reinterpret_cast<const uint2*>(base + (g << 3));
+                v[u][0] = x.x; v[u][1] = x.y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(base + (((g + 8 * j) ^ (SWZ ? r & 7 : 0)) << 4));
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[u][4 * j + w] = word(x, w);
+                }
+            }
+        }
+        if (gone)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if ((gone >> (2 * t + (u & 1) + 8 * (u >> 1))) & 1u)
+#pragma unroll
+                    for (int j = 0; j < VB; ++j) v[u][j] = 0u;
+        const uint32_t hi0 = pack_bf16(p[0], p[1]), hi1 = pack_bf16(p[2], p[3]);
+        const uint32_t lo0 = pack_bf16(p[0] - __uint_as_float(hi0 << 16), p[1] - __uint_as_float(hi0 & 0xffff0000u));
+        const uint32_t lo1 = pack_bf16(p[2] - __uint_as_float(hi1 << 16), p[3] - __uint_as_float(hi1 & 0xffff0000u));
         const uint32_t h0 = movmatrix_trans(hi0), h1 = movmatrix_trans(hi1), e0 = movmatrix_trans(lo0), e1 = movmatrix_trans(lo1);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -147,7 +147,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
         }
     }
     static __device__ __forceinline__ void finish(Acc&) {}
-    static __device__ __forceinline__ int rho(int g) { return g; }
     static __device__ __forceinline__ int channel(int m, int g) { return D == 32 ? g * 4 + 2 * m : (m >> 2) * 64 + g * 8 + 2 * (m & 3); }
 };
 
@@ -193,9 +192,9 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3) + 4);
         }
     }
-    // keys, parameters: of this span's first row
-    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* keys, const unsigned char* pars, int g, int t)
+    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* st, int span, int g, int t)
     {
+        const unsigned char *keys = st + Stage<D, true>::K + span * (8 * D), *pars = st + Stage<D, true>::KP + span * (64 * GR);
         const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
         uint32_t k[2][GR], kp[2][GR];
 #pragma unroll
@@ -233,9 +232,9 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
     }
-    // gone: bit 0, 1: the rows of M-rows g, g + 8 do not count
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* values, const unsigned char* pars, unsigned gone, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* st, int span, unsigned gone, int g, int t)
     {
+        const unsigned char *values = st + Stage<D, true>::V + span * (8 * D), *pars = st + Stage<D, true>::VP + span * (64 * GR);
         const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
         uint32_t v[4][(GR + 1) / 2], vp[2][GR];
 #pragma unroll
@@ -246,12 +245,12 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) get<Words>(vp[u], pars + (rho(g) + 8 * u) * (4 * GR));
-        if (gone & 1u)
+        if (gone)
 #pragma unroll
-            for (int j = 0; j < GR; ++j) vp[0][j] = 0u;
-        if (gone & 2u)
+            for (int u = 0; u < 2; ++u)
+                if ((gone >> (rho(g) + 8 * u)) & 1u)
 #pragma unroll
-            for (int j = 0; j < GR; ++j) vp[1][j] = 0u;
+                    for (int j = 0; j < GR; ++j) vp[u][j] = 0u;
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
             const float s0 = par4_step(vp[0][j]), s1 = par4_step(vp[1][j]);
@@ -289,13 +288,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
 };
 
-// Stages of shared memory through which a warp's units of a cache in 4 bits pass: bulk copies that the warp's lane 0 starts, a barrier per stage.
-// (In registers, as bf16 rows are, enough units in flight and the products' operands do not fit 128 registers, and every load costs
-// its address arithmetic in every lane.)
-template <int D> struct Stage4 {
-    static constexpr int UR = 32, STAGES = 3, K = 0, V = UR * D / 2, KP = 2 * V, VP = KP + UR * D / 8, BYTES = VP + UR * D / 8;
-};
-
 __device__ StatusWord g_rows_status = LTE_STATUS_INIT;
 
 __device__ __forceinline__ void bulk_copy(uint32_t to, const unsigned char* from, uint32_t bytes, uint32_t bar)
@@ -304,28 +296,25 @@ __device__ __forceinline__ void bulk_copy(uint32_t to, const unsigned char* from
 }
 
 template <int D, int NW, bool SWZ, bool FOUR, bool ACCUM>
-__global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma_kernel(
+__global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
     float scale, int G, int most)                              // most: rows whose logits a warp keeps (whole spans)
 {
     using Gr = Group<D, SWZ, FOUR>;
     constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
-    // A warp takes UNIT spans at a time, NBUF times as many in flight.  (4 bits: two at a time, so that instructions of one fill the other's
-    // latencies; bf16 waits for memory.)
-    constexpr int UNIT = FOUR ? 2 : 1, UR = 16 * UNIT;
-    using St = Stage4<D>;
-    constexpr int NBUF = FOUR ? St::STAGES : 2;
+    using St = Stage<D, FOUR>;
+    constexpr int UR = St::UR, UNIT = UR / 16;
     constexpr int SPLIT = NW == max_warps(D) ? MAX_SPLIT : 1;  // (only the largest blocks come in clusters)
-    extern __shared__ __align__(128) unsigned char s_dyn[];    // 4 bits: the warps' stages; [NW][most][nq] logits, behind them [NW][most] sums over passes
-    float* const s_log = reinterpret_cast<float*>(s_dyn + (FOUR ? NW * St::STAGES * St::BYTES : 0));
-    __shared__ __align__(8) uint64_t s_bar[FOUR ? NW * St::STAGES : 1];
-    __shared__ __align__(16) float s_acc[NW][MQ][PITCH];
+    extern __shared__ __align__(128) unsigned char s_dyn[];    // the warps' stages; [NW][most][nq] logits, behind them [NW][most] sums over passes
+    float* const s_log = reinterpret_cast<float*>(s_dyn + NW * St::STAGES * St::BYTES);
+    auto s_acc = [&](int w, int u) { return reinterpret_cast<float*>(s_dyn + w * (St::STAGES * St::BYTES)) + u * PITCH; };
+    __shared__ __align__(8) uint64_t s_bar[NW * St::STAGES];
     __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
     __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
     __shared__ __align__(16) float s_ml[2][SPLIT][MQ][2];      // the cluster's shares of this block's output elements (by pass parity)
     __shared__ __align__(16) __nv_bfloat16 s_kv[2][D];         // the incoming token
-    __shared__ float s_tap[kMaxTaps];
+    __shared__ float s_tap[NW];
     __shared__ uint32_t s_wkey[NW];
     __shared__ int s_wpos[NW], s_wslot[NW];
     cg::cluster_group cluster = cg::this_cluster();
@@ -339,13 +328,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
     const bool shared_head = SPLIT > 1 && nsplit > 1;          // (uniform in the cluster)
     if (shared_head) cluster.barrier_arrive();                 // (awaited before the first store into another block's shared memory)
     pdl_launch_dependents();
-    if constexpr (FOUR) {
-        if (lane == 0) {
-            for (int i = 0; i < St::STAGES; ++i) tc::mbar_init(tc::smem_u32(&s_bar[wid * St::STAGES + i]), 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncwarp();
+    if (lane == 0) {
+        for (int i = 0; i < St::STAGES; ++i) tc::mbar_init(tc::smem_u32(&s_bar[wid * St::STAGES + i]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncwarp();
     pdl_wait();
 
     // Everything whose address is known is asked for at once: the rows that a warp begins with too, whether or not they turn out to be in use.
@@ -353,35 +340,26 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
     rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
     rows.total = W + R;
     const int step = NW * nsplit, first = wid * nsplit + rank;
-    // bf16: registers
-    Gr buf[FOUR ? 1 : NBUF];
-    auto load_k = [&](Gr& u, int i) { if constexpr (!FOUR) { if (UR * (i + 1) <= rows.total) u.template load_k<true>(rows, i, g, t); else u.template load_k<false>(rows, i, g, t); } };
-    auto load_v = [&](Gr& u, int i) { if constexpr (!FOUR) { if (UR * (i + 1) <= rows.total) u.template load_v<true>(rows, i, g, t); else u.template load_v<false>(rows, i, g, t); } };
-    // 4 bits: unit number j of this warp goes through stage j % STAGES; `asked` and `taken` count over all passes
     unsigned char* const stage = s_dyn + wid * (St::STAGES * St::BYTES);
-    const uint32_t bar = tc::smem_u32(&s_bar[FOUR ? wid * St::STAGES : 0]);
-    int asked = 0, taken = 0;
+    const uint32_t bar = tc::smem_u32(&s_bar[wid * St::STAGES]);
+    int asked = 0, taken = 0;                                  // units of this warp, over all passes: number j goes through stage j % STAGES
     auto ask = [&](int i) {
-        if constexpr (FOUR) {
-            if (lane == 0) {
-                const uint32_t nr = min(UR, rows.total - UR * i), row = nr * (D / 2), par = (nr * (4 * GR) + 15) & ~15u;   // (a part's size in the cache is a multiple of 16)
-                const uint32_t b = bar + 8 * (asked % St::STAGES), to = tc::smem_u32(stage + (asked % St::STAGES) * St::BYTES);
-                tc::mbar_expect_tx(b, 2 * (row + par));
-                bulk_copy(to + St::K, rows.K + (size_t)i * (UR * D / 2), row, b);
-                bulk_copy(to + St::KP, rows.KP + (size_t)i * (UR * 4 * GR), par, b);
-                bulk_copy(to + St::V, rows.V + (size_t)i * (UR * D / 2), row, b);
-                bulk_copy(to + St::VP, rows.VP + (size_t)i * (UR * 4 * GR), par, b);
-            }
-            ++asked;
+        if (lane == 0) {
+            const uint32_t nr = min(UR, rows.total - UR * i), row = nr * St::ROW, par = (nr * St::PAR + 15) & ~15u;   // (a part's size in the cache is a multiple of 16)
+            const uint32_t b = bar + 8 * (asked % St::STAGES), to = tc::smem_u32(stage + (asked % St::STAGES) * St::BYTES);
+            tc::mbar_expect_tx(b, 2 * (row + par));
+            bulk_copy(to + St::K, rows.K + (size_t)i * (UR * St::ROW), row, b);
+            if (FOUR) bulk_copy(to + St::KP, rows.KP + (size_t)i * (UR * St::PAR), par, b);
+            bulk_copy(to + St::V, rows.V + (size_t)i * (UR * St::ROW), row, b);
+            if (FOUR) bulk_copy(to + St::VP, rows.VP + (size_t)i * (UR * St::PAR), par, b);
         }
+        ++asked;
     };
+    auto wait = [&](int code) { tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, code, &g_rows_status); };
     auto begin = [&](int units_there) {                        // the first units of a pass
 #pragma unroll
-        for (int b = 0; b < NBUF; ++b)
-            if (first + b * step < units_there) {
-                if constexpr (FOUR) ask(first + b * step);
-                else { load_k(buf[b], first + b * step); load_v(buf[b], first + b * step); }
-            }
+        for (int b = 0; b < St::STAGES; ++b)
+            if (first + b * step < units_there) ask(first + b * step);
     };
     begin((rows.total + UR - 1) / UR);
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
@@ -397,37 +375,58 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         pp[u] = m < R ? pidx[m] : -1;
     }
     if (tid < D / 4) reinterpret_cast<uint4*>(s_kv)[tid] = reinterpret_cast<const uint4*>((tid < D / 8 ? k1 : v1) + (size_t)bh * D)[tid % (D / 8)];
-    float wk[CPL], wv[CPL];                                    // scorer weights of tap `wid` (the first block scores)
-    const bool taps = !ACCUM && rank == 0 && wid < rule.K;
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) {
-        wk[c] = taps ? rule.w[((size_t)h * rule.K + wid) * 2 * D + lane + 32 * c] : 0.f;
-        wv[c] = taps ? rule.w[((size_t)h * rule.K + wid) * 2 * D + D + lane + 32 * c] : 0.f;
-    }
     const int slot = n % W, p = n - W, half = rule.K / 2;
     rows.total = n < W ? n : W + cnt_old;
     const int units = (rows.total + UR - 1) / UR, full = rows.total / UR;
     const float zp = p >= 0 ? zc[slot] : 0.f;
-    // learned rule: channels lane, lane + 32, .. of the row under a tap, as the cache holds it
+    // Learned rule, the first block: logit of the newest token whose receptive field is complete.  A lane takes eight channels under a tap: a
+    // word of the row's key or value codes, two runs of four weights.
     const int jsc = ACCUM ? -1 : n - half;
-    auto tap_rows = [&](int tap, float (&kx)[CPL], float (&vx)[CPL]) {
-        const int pos = jsc + tap - half, r = pos < 0 ? 0 : pos % W;
+    constexpr int LT = D / 4, TAPS = 32 / LT;                  // lanes per tap, taps of a warp at a time
+    struct Tap { uint4 x; float w[8]; uint32_t par[2]; bool held; };
+    const int tap_word = lane % LT % (D / 8), tap_values = lane % LT / (D / 8);
+    auto tap_ask = [&](Tap& T, int tap) {
+        const int pos = n - (rule.K - 1) + tap;                // (the ring holds at least K tokens)
+        T.held = pos != n;
+        T.x = make_uint4(0, 0, 0, 0);
+        T.par[0] = T.par[1] = 0u;
 #pragma unroll
-        for (int c = 0; c < CPL; ++c) {
-            kx[c] = vx[c] = 0.f;
-            if (pos == n) {
-                kx[c] = __bfloat162float(k1[(size_t)bh * D + lane + 32 * c]);
-                vx[c] = __bfloat162float(v1[(size_t)bh * D + lane + 32 * c]);
-            } else if (pos >= 0) {
-                const uint32_t kw = reinterpret_cast<const uint32_t*>(rows.K + (size_t)r * (D / 2))[(lane >> 3) * GR + c];
-                const uint32_t vw = reinterpret_cast<const uint16_t*>(rows.V + (size_t)r * (D / 2))[(lane >> 2) * GR + c];
-                kx[c] = value4((kw >> (4 * (lane & 7))) & 15u, reinterpret_cast<const uint32_t*>(rows.KP)[(size_t)r * GR + c]);
-                vx[c] = value4((vw >> (4 * (lane & 3))) & 15u, reinterpret_cast<const uint32_t*>(rows.VP)[(size_t)r * GR + c]);
-            }
+        for (int e = 0; e < 8; ++e) T.w[e] = 0.f;
+        if (tap >= rule.K || pos < 0) return;
+        const int ch0 = tap_values ? value4_channel(tap_word, 0, GR) : key4_channel(tap_word, 0, GR);
+        const int ch4 = tap_values ? value4_channel(tap_word, 4, GR) : key4_channel(tap_word, 4, GR);
+        const float* w = rule.w + ((size_t)h * rule.K + tap) * 2 * D + tap_values * D;
+        if ((reinterpret_cast<uintptr_t>(rule.w) & 15u) == 0) {
+            const float4 a = *reinterpret_cast<const float4*>(w + ch0), b = *reinterpret_cast<const float4*>(w + ch4);
+            T.w[0] = a.x; T.w[1] = a.y; T.w[2] = a.z; T.w[3] = a.w; T.w[4] = b.x; T.w[5] = b.y; T.w[6] = b.z; T.w[7] = b.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { T.w[e] = w[ch0 + e]; T.w[4 + e] = w[ch4 + e]; }
+        }
+        if (T.held) {
+            const int back = slot + tap - (rule.K - 1), r = back < 0 ? back + W : back;
+            T.x.x = reinterpret_cast<const uint32_t*>((tap_values ? rows.V : rows.K) + (size_t)r * (D / 2))[tap_word];
+            const uint32_t* par = reinterpret_cast<const uint32_t*>(tap_values ? rows.VP : rows.KP) + (size_t)r * GR;
+            T.par[0] = par[ch0 / kGroup4]; T.par[1] = par[ch4 / kGroup4];
+        } else {                                               // the incoming token, as given
+            const __nv_bfloat16* x = (tap_values ? v1 : k1) + (size_t)bh * D;
+            const uint2 a = *reinterpret_cast<const uint2*>(x + ch0), b = *reinterpret_cast<const uint2*>(x + ch4);
+            T.x = make_uint4(a.x, a.y, b.x, b.y);
         }
     };
-    float kx[CPL], vx[CPL];
-    if (taps && jsc >= 0) tap_rows(wid, kx, vx);
+    auto tap_sum = [&](const Tap& T) {
+        float a = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t u = word(T.x, e >> 1);
+            const float x = T.held ? value4((T.x.x >> (4 * e)) & 15u, T.par[e >> 2]) : __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
+            a = fmaf(T.w[e], x, a);
+        }
+        return a;
+    };
+    Tap tap0;
+    const bool scores = !ACCUM && rank == 0 && jsc >= 0;
+    if (scores) tap_ask(tap0, wid * TAPS + lane / LT);
 
     // ---- what happens to the token leaving the window ------------------------------------------------------------
     int dst = -1, cnt_new = cnt_old;
@@ -451,23 +450,14 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
     const int masked_ring = p >= 0 && dst < 0 ? slot : -32;    // the popped row counts iff the pool takes it ...
     const int masked_pool = dst >= 0 && dst < cnt_old ? W + dst : -32;   // ... and then the entry it replaces does not
 
-    // ---- learned rule, the first block: logit of the newest token whose receptive field is complete -----------------
-    if (!ACCUM && rank == 0 && jsc >= 0) {
-        for (int tap = wid; tap < rule.K; tap += NW) {
-            if (tap >= NW) {
-                tap_rows(tap, kx, vx);
-#pragma unroll
-                for (int c = 0; c < CPL; ++c) {
-                    wk[c] = rule.w[((size_t)h * rule.K + tap) * 2 * D + lane + 32 * c];
-                    wv[c] = rule.w[((size_t)h * rule.K + tap) * 2 * D + D + lane + 32 * c];
-                }
-            }
-            float a = 0.f;
-#pragma unroll
-            for (int c = 0; c < CPL; ++c) a += wk[c] * kx[c] + wv[c] * vx[c];
-            a = warp_sum(a);
-            if (lane == 0) s_tap[tap] = a;
+    if (scores) {
+        float a = tap_sum(tap0);
+        for (int tap = (wid + NW) * TAPS; tap < rule.K; tap += NW * TAPS) {
+            tap_ask(tap0, tap + lane / LT);
+            a += tap_sum(tap0);
         }
+        a = warp_sum(a);
+        if (lane == 0) s_tap[wid] = a;
     }
 
     // the popped row's words, read before the slot is written: thread e of the last ones moves word e
@@ -496,6 +486,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         const int nq = min(MQ, G - g0);
         if (g0 > 0) {                                          // further query heads read the rows again
             Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
+            __syncthreads();                                   // the previous pass's outputs, which stand in the stages, have been combined
+            tc::fence_proxy_async();
             begin(units);
         }
         typename Gr::Acc acc;
@@ -503,27 +495,22 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
         int kept = 0;                                          // rows whose logits this warp has kept
 
-        // one unit; its registers (or its stage) are refilled with the warp's unit NBUF steps ahead as soon as the products have taken them
-        auto compute = [&](int b, int i) {
-            const int next = i + NBUF * step;
+#pragma unroll 1
+        for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
-            const unsigned char* at4 = stage + (taken % St::STAGES) * St::BYTES;
-            if constexpr (FOUR) {
-                tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, 1, &g_rows_status);
+            const unsigned char* st = stage + (taken % St::STAGES) * St::BYTES;
+            wait(1);
 #pragma unroll
-                for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, at4 + St::K + x * (8 * D), at4 + St::KP + x * (64 * GR), g, t);
-            } else {
-                buf[b].logits(c[0], qf);
-                if (next < units) load_k(buf[b], next);
-            }
-            unsigned gone[UNIT] = {};
+            for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
+            unsigned gone = 0;                                 // rows of the unit that do not count
             if (i >= full || i == masked_ring / UR || i == masked_pool / UR) {
+                if (i >= full) gone = ~0u << (rows.total - UR * i);
+                if (i == masked_ring / UR) gone |= 1u << (masked_ring % UR);
+                if (i == masked_pool / UR) gone |= 1u << (masked_pool % UR);
 #pragma unroll
                 for (int x = 0; x < UNIT; ++x) {
-                    auto out = [&](int r) { const int row = UR * i + 16 * x + r; return row >= rows.total || row == masked_ring || row == masked_pool; };
-                    if (out(Gr::rho(g))) { c[x][0] = c[x][1] = -INFINITY; gone[x] |= 1u; }
-                    if (out(Gr::rho(g) + 8)) { c[x][2] = c[x][3] = -INFINITY; gone[x] |= 2u; }
-                    if constexpr (!FOUR) buf[b].clear(out, g, t);
+                    if ((gone >> (16 * x + Gr::rho(g))) & 1u) c[x][0] = c[x][1] = -INFINITY;
+                    if ((gone >> (16 * x + Gr::rho(g) + 8)) & 1u) c[x][2] = c[x][3] = -INFINITY;
                 }
             }
             if constexpr (ACCUM) {                             // raw logits [row][query]
@@ -559,29 +546,13 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
                 for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast((c[x][e] - (e & 1 ? m1 : m0)) * scale2);
                 l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3];
             }
-            if constexpr (FOUR) {
 #pragma unroll
-                for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], at4 + St::V + x * (8 * D), at4 + St::VP + x * (64 * GR), gone[x], g, t);
-                ++taken;
-                __syncwarp();                                  // every lane has read the stage
-                if (next < units) ask(next);
-            } else {
-                buf[b].output(acc, p[0][0], p[0][1], p[0][2], p[0][3]);
-                if (next < units) load_v(buf[b], next);
-            }
-        };
-        if constexpr (FOUR) {
-#pragma unroll 1
-            for (int i = first; i < units; i += step) compute(0, i);
-            for (; taken < asked; ++taken)                     // units asked for before it was known how many rows are in use
-                tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, 2, &g_rows_status);
-        } else {
-            for (int i = first; i < units; i += NBUF * step) {
-#pragma unroll
-                for (int b = 0; b < NBUF; ++b)
-                    if (i + b * step < units) compute(b, i + b * step);
-            }
+            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
+            ++taken;
+            __syncwarp();                                      // every lane has read the stage
+            if (i + St::STAGES * step < units) ask(i + St::STAGES * step);
         }
+        for (; taken < asked; ++taken) wait(2);                // units asked for before it was known how many rows are in use
         const bool last = g0 + MQ >= G;
         if (rank == 0 && last && dst >= 0)                     // (back by the time the write-back needs them)
 #pragma unroll
@@ -608,8 +579,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int ch = Gr::channel(i, g);
-            if (2 * t < nq) *reinterpret_cast<float2*>(&s_acc[wid][2 * t][ch]) = make_float2(acc.a[i][0], acc.a[i][2]);
-            if (2 * t + 1 < nq) *reinterpret_cast<float2*>(&s_acc[wid][2 * t + 1][ch]) = make_float2(acc.a[i][1], acc.a[i][3]);
+            if (2 * t < nq) *reinterpret_cast<float2*>(&s_acc(wid, 2 * t)[ch]) = make_float2(acc.a[i][0], acc.a[i][2]);
+            if (2 * t + 1 < nq) *reinterpret_cast<float2*>(&s_acc(wid, 2 * t + 1)[ch]) = make_float2(acc.a[i][1], acc.a[i][3]);
         }
         if (rank == 0)                                         // the incoming token's logits
             for (int u = wid; u < nq; u += NW) {
@@ -638,7 +609,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
             block_sum(u, m, tot);
             float o = rank == 0 ? exp2_fast((s_new[u] - m) * scale2) * __bfloat162float(s_kv[1][ch]) : 0.f;
 #pragma unroll
-            for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_acc[w2][u][ch], o);
+            for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_acc(w2, u)[ch], o);
             if (!shared_head) {
                 o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
                 if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * scale + logf(tot);
@@ -745,9 +716,10 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_rows_mma
         } else {
             if (dst >= 0) zc[W + dst] = zp;
             float znew = rule.bias ? rule.bias[h] : 0.f;
-            if (jsc >= 0) for (int tap = 0; tap < rule.K; ++tap) znew += s_tap[tap];
+            if (jsc >= 0)
+                for (int w = 0; w < NW; ++w) znew += s_tap[w];
             zc[slot] = -INFINITY;                              // the incoming token is not scored yet ...
-            if (jsc >= 0) zc[jsc % W] = znew;                  // ... unless K == 1 (then jsc == n)
+            if (jsc >= 0) zc[slot - half < 0 ? slot - half + W : slot - half] = znew;   // ... unless K == 1 (then jsc == n)
         }
         meta[0] = n + 1;
         meta[1] = cnt_new;
@@ -762,14 +734,14 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
 {
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
-    const int BH = p.B * p.H, rows = p.W + p.R, warps = warps_per_sm(p.d) * n_sm, most_w = max_warps(p.d);
-    constexpr int UR = FOUR ? 32 : 16;                         // rows that a warp takes at a time
+    const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm, most_w = max_warps(p.d);
+    constexpr int UR = Stage<64, FOUR>::UR;                    // rows that a warp takes at a time
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
     auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
     auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };   // of logits
     int nw = 1, nsplit = 1;
     for (int c : {2, 4, 8})
-        if (c <= most_w && ((BH <= n_sm * (warps_per_sm(p.d) / c) && rows / c >= 16) || smem(c / 2, 1) * (warps_per_sm(p.d) / (c / 2)) > 128 * 1024)) nw = c;
+        if (c <= most_w && ((BH <= n_sm * (wps / c) && rows / c >= 16) || smem(c / 2, 1) * (wps / (c / 2)) > 96 * 1024)) nw = c;
     if (nw == most_w)
         while (nsplit < MAX_SPLIT && ((BH * nw * nsplit * 2 <= warps && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
     auto go = [&](auto d, auto w, auto s) {
@@ -777,9 +749,9 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         if constexpr (NW <= max_warps(D)) {
             auto kern = decode_rows_mma_kernel<D, NW, decltype(s)::value, FOUR, ACCUM>;
             static PerDeviceOnce once;
-            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 192 * 1024); })) return e;
+            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); })) return e;
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit) + (FOUR ? NW * Stage4<D>::STAGES * Stage4<D>::BYTES : 0);
+            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit) + NW * Stage<D, FOUR>::STAGES * Stage<D, FOUR>::BYTES;
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
             attr[0].val.programmaticStreamSerializationAllowed = 1;
