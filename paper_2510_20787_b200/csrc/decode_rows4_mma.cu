@@ -11,6 +11,4 @@ int launch_decode_rows4_bf16(const Params& p, bool accum, const RowsRule& rule, 
                  : launch_rows_mma<true, false>(p, L, false, rule, cache, q1, k1, v1, o1, lse1, st);
 }
 
-int decode_rows4_status_fetch_and_clear() { return status_fetch_and_clear(g_rows_status); }
-
 }  // namespace lte

@@ -10,6 +10,4 @@ int launch_decode_rows_bf16(const Params& p, const RowsRule& rule, void* cache, 
     return launch_rows_mma<false, true>(p, rows_layout(C), C.swz != 0, rule, cache, q1, k1, v1, o1, lse1, st);
 }
 
-int decode_rows_status_fetch_and_clear() { return status_fetch_and_clear(g_rows_status); }
-
 }  // namespace lte

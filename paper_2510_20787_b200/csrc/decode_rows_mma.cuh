@@ -1,27 +1,29 @@
 // Decode step (lte_attn_decode_accum, lte_attn_decode4, lte_attn_decode4_accum) for bf16 calls: rows go from memory straight into tensor-core
 // operands, as in decode_mma.cu, every query head of a group at once, heads split over warps and clusters where there are few.
 //
-// Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there unpacking and memory are about even.  Every warp
-// walks spans of 16 rows (interleaved over the warps of all blocks that share the head) with NBUF spans in flight, keeps its own
-// reference, sum and output, and meets the others once at the end.  The incoming token is no row: its logit is a dot product on the fp32 ALUs, and it
-// joins where the warps meet.
+// Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there the instructions that unpack and weigh them count for more
+// (see the figures at the launch).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
+// through stages of its own in shared memory, keeps its own reference, sum and output, and meets the others once at the end.  The incoming token
+// is no row: its logit is a dot product on the fp32 ALUs, and it joins where the warps meet.
 //
 // Scores (accumulated attention): a row's weight needs the sum over all rows, so the raw logits of a warp's rows stay in shared memory until the
 // blocks have met; then every warp adds its rows' weights, summed over the query heads, to their scores.  One read and one write of 4 bytes a row.
 //
 // Products are mma.sync m16n8k16: logits S^T[16 rows][8 queries] = K q^T, output O^T[16 channels][8 queries] += V^T P^T, N = 8 queries.
-// Rows in 4 bits.  A code c becomes the bf16 number 16 + c by a shift and one three-input logic operation on two codes at a time (the code is
-// the top of the mantissa): exact, no conversion.  With value = zero + c step = (zero - 16 step) + step (16 + c):
-//   logits   per group of 32 channels, step (16 + c).q + (zero - 16 step) sum(q): the group's product starts from zero, and its two scalars,
-//            which belong to a row, are applied to the products in fp32 (a lane holds rows g and g + 8 of both);
-//   output   P step takes the place of P, per group, and P (zero - 16 step), which is the same for all channels of a group, is summed beside it.
+// Rows in 4 bits.  A code is an fp16 number as it stands: the low ten bits of a half are its fraction, so that c in bits 0-3 is the subnormal number
+// c 2^-24, in bits 4-7 16 c 2^-24; a mask on two codes at a time is all the conversion there is.  With value = zero + c step:
+//   logits   per group of 32 channels, step c.q + zero sum(q): the group's product starts from zero, and its two scalars, which belong to a
+//            row, are applied to the products in fp32 (a lane holds rows of both).  q is scaled by a power of two per query head to at most 2^15 (and
+//            by 1/16 where it meets 16 c), in which fp16 holds bf16 numbers exactly down to 2^-24; logits are kept in that scale;
+//   output   P step takes the place of P, per group, and P zero, the same for all channels of a group, is summed beside it in fp32.  P step is
+//            rounded to fp16, 2^-12 of it: an error of o of at most 2^-12 sum(w c step), a tenth of the rounding of o itself in the mean square (o
+//            against 64 bits: 1.7e-3 before and after).  It is scaled by a power of two, the same for the warp, that follows the largest step.
 // The contraction index may be permuted freely: the nibbles i and i + 4 of a key word are neighbours in it, and so are the two rows whose value
 // units a byte permute joins.  The order of the codes in the cache (cache4.cuh) makes these the words that a lane loads.
-// P (times step) is split into two bf16 terms: 16 bits of mantissa.  With one term o would be off by more than its own rounding: the 16 + c
-// are all positive, so that o is the small difference of sums as large as the rows.
 #pragma once
 #include <cfloat>
 #include <cooperative_groups.h>
+#include <cuda_fp16.h>
 
 #include <type_traits>
 
@@ -36,13 +38,14 @@ namespace {
 constexpr int MQ = 8;                                          // query heads per pass
 // resident warps the registers (and the stages in shared memory) are budgeted for
 __host__ __device__ constexpr int warps_per_sm(int d, bool four) { return d == 128 ? 8 : 16; }
-__host__ __device__ constexpr int max_warps(int d) { return d == 128 ? 4 : 8; }       // per block
-constexpr int MAX_SPLIT = 8;                                   // blocks per head
+constexpr int MAX_WARPS = 8;                                   // per block
+// blocks of so many warps come in clusters (at d = 128 eight warps take an SM's registers, and the next step's blocks then find no room beside them)
+__host__ __device__ constexpr bool clusters(int d, int nw) { return nw == MAX_WARPS || (d == 128 && nw == 4); }
+constexpr int MAX_SPLIT = 16;                                  // blocks per head
 
 // A head's rows in use are rows 0 .. total - 1 of its block (while the ring fills up the pool is empty).  A warp takes units of UR of them, 16 to
-// a product, which pass through STAGES of its own in shared memory: bulk copies that its lane 0 starts, a barrier per stage.  (With the units in
-// registers, enough of them in flight and the products' operands did not fit 128 registers, and every load cost its address arithmetic in
-// every lane: 256 heads x 1,280 rows in 4 bits 23.7 us, through shared memory 18.5.)
+// a product, which pass through STAGES of its own in shared memory by 16-byte asynchronous copies.  (With the units in registers, enough of them
+// in flight and the products' operands did not fit 128 registers: 256 heads x 1,280 rows in 4 bits 23.7 us, through shared memory 18.5.)
 struct Rows {
     const unsigned char *K, *V, *KP, *VP;
     int total;
@@ -61,13 +64,19 @@ template <int D, bool SWZ, bool FOUR> struct Group;
 
 template <int D, bool SWZ> struct Group<D, SWZ, false> {
     static constexpr int KP = D / 32, VB = D / 16, PITCH = D * 2, MT = D / 16;
-    struct Query { uint4 f[KP]; };                             // pieces t, t + 4, .. of query g
+    static constexpr float LIFT = 1.f;
+    struct Query { uint4 f[KP]; float unit[2]; };              // pieces t, t + 4, .. of query g
     struct Acc { float a[MT][4]; };
+    struct Pars {};
+    static __device__ __forceinline__ float load_pars(Pars&, const unsigned char*, int, unsigned, int) { return 0.f; }
+    static __device__ __forceinline__ bool too_large(const Acc&, float) { return false; }
+    static __device__ __forceinline__ void lower(Acc&, float) {}
     static __device__ __forceinline__ int rho(int g) { return g; }
     static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
     {
 #pragma unroll
         for (int j = 0; j < KP; ++j) Q.f[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
+        Q.unit[0] = Q.unit[1] = 1.f;
     }
     // c: rows g (0, 1) and g + 8 (2, 3), queries 2t and 2t + 1.  A product rounds its running sum towards zero, so every one starts from zero
     // and the parts are added to the nearest (see decode_mma.cu).  Lane (g, t) takes pieces t, t + 4, .. of rows g and g + 8.
@@ -109,7 +118,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
         for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
     }
     // gone: bit r: row r of the span does not count.  Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* st, int span, unsigned gone, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, const unsigned char* st, int span, unsigned gone, int g, int t)
     {
         uint32_t v[4][VB];
 #pragma unroll
@@ -150,23 +159,14 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     static __device__ __forceinline__ int channel(int m, int g) { return D == 32 ? g * 4 + 2 * m : (m >> 2) * 64 + g * 8 + 2 * (m & 3); }
 };
 
-// two codes of a word, at bits 4i and 4i + 16, as the bf16 numbers 16 + c
-// (one LOP3: with both constants as immediates the compiler takes two)
-__device__ __forceinline__ uint32_t reg(uint32_t x) { asm("" : "+r"(x)); return x; }
-template <int I> __device__ __forceinline__ uint32_t codes2(uint32_t x, uint32_t mask, uint32_t sixteen)
-{
-    const uint32_t y = I == 0 ? x << 3 : x >> (4 * I - 3);
-    uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(y), "r"(mask), "r"(sixteen));     // (y & mask) | sixteen
-    return r;
-}
-
 // Rows in 4 bits: a span stands in shared memory, where the products take their operands from.  M-row r of a product is row rho(r) of the span,
 // rho(2t + b + 8c) = t + 4b + 8c: the value units that the lanes load at once then lie in different banks.
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static constexpr int GR = D / kGroup4, MT = D / 16;
-    struct Query { uint32_t f[GR][4]; float sum[GR][2]; };     // of query g; sums of queries 2t, 2t + 1 over a group's channels
-    struct Acc { float a[MT][4], z[GR][2]; };
+    static constexpr float LIFT = 16777216.f;                  // 2^24: logits are kept as sums of c 2^-24 q
+    struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and inverse scales of queries 2t, 2t + 1
+    struct Acc { float a[MT][4], z[GR][2], inv; };             // inv: the scale of P step
+    struct Pars { uint32_t p[2][GR]; };                        // of rows rho(g), rho(g) + 8
     template <typename U> static __device__ __forceinline__ void get(uint32_t (&x)[GR], const unsigned char* p)
     {
         const U u = *reinterpret_cast<const U*>(p);
@@ -177,25 +177,45 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static __device__ __forceinline__ int rho(int g) { return (g >> 1) + 4 * (g & 1); }     // (g < 8)
     static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
     {
-        const int lane = 4 * g + t;
+        uint4 u[GR];
+        float top = 0.f;
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
-            const uint4 u = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D + j * kGroup4)[t] : make_uint4(0, 0, 0, 0);
-            Q.f[j][0] = __byte_perm(u.x, u.z, 0x5410); Q.f[j][1] = __byte_perm(u.x, u.z, 0x7632);   // channels 0, 4 | 1, 5
-            Q.f[j][2] = __byte_perm(u.y, u.w, 0x5410); Q.f[j][3] = __byte_perm(u.y, u.w, 0x7632);   // 2, 6 | 3, 7
-            float s = 0.f;
+            u[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D + j * kGroup4)[t] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) s += __uint_as_float(word(u, w) << 16) + __uint_as_float(word(u, w) & 0xffff0000u);
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(word(u[j], w) << 16)), fabsf(__uint_as_float(word(u[j], w) & 0xffff0000u))));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // the power of two that takes the largest channel to 2^14 .. 2^15 (1 for a query that is zero or not finite)
+        const uint32_t ex = __float_as_uint(top) >> 23, field = top > 0.f && top < INFINITY ? min(268u - ex, 253u) : 127u;
+        const float scale = __uint_as_float(field << 23), unit = __uint_as_float((254u - field) << 23);
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+            float x[8], s = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                x[2 * w] = __uint_as_float(word(u[j], w) << 16) * scale;
+                x[2 * w + 1] = __uint_as_float(word(u[j], w) & 0xffff0000u) * scale;
+                s += x[2 * w] + x[2 * w + 1];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                      // channels i and i + 4
+                const __half2 h = i & 1 ? __floats2half2_rn(x[i] * 0.0625f, x[i + 4] * 0.0625f) : __floats2half2_rn(x[i], x[i + 4]);
+                Q.f[j][i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
             s += __shfl_xor_sync(0xffffffffu, s, 1);
             s += __shfl_xor_sync(0xffffffffu, s, 2);
-            Q.sum[j][0] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3));
-            Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * (lane & 3) + 4);
+            s *= 1.f / LIFT;
+            Q.sum[j][0] = __shfl_sync(0xffffffffu, s, 8 * t);
+            Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
         }
+        Q.unit[0] = __shfl_sync(0xffffffffu, unit, 8 * t);
+        Q.unit[1] = __shfl_sync(0xffffffffu, unit, 8 * t + 4);
     }
     static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* st, int span, int g, int t)
     {
         const unsigned char *keys = st + Stage<D, true>::K + span * (8 * D), *pars = st + Stage<D, true>::KP + span * (64 * GR);
-        const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
         uint32_t k[2][GR], kp[2][GR];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -205,15 +225,16 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
             float p[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816(p, codes2<0>(k[0][j], M, S), codes2<0>(k[1][j], M, S), codes2<1>(k[0][j], M, S), codes2<1>(k[1][j], M, S), Q.f[j][0], Q.f[j][1]);
-            mma16816(p, codes2<2>(k[0][j], M, S), codes2<2>(k[1][j], M, S), codes2<3>(k[0][j], M, S), codes2<3>(k[1][j], M, S), Q.f[j][2], Q.f[j][3]);
+            const uint32_t x = k[0][j], y = k[1][j], x8 = x >> 8, y8 = y >> 8;
+            mma16816_f16(p, x & 0x000f000fu, y & 0x000f000fu, x & 0x00f000f0u, y & 0x00f000f0u, Q.f[j][0], Q.f[j][1]);
+            mma16816_f16(p, x8 & 0x000f000fu, y8 & 0x000f000fu, x8 & 0x00f000f0u, y8 & 0x00f000f0u, Q.f[j][2], Q.f[j][3]);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float s = par4_step(kp[i][j]), z = fmaf(-16.f, s, par4_zero(kp[i][j]));
+                const float s = par4_step(kp[i][j]), z = par4_zero(kp[i][j]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float x = fmaf(s, p[2 * i + e], z * Q.sum[j][e]);
-                    c[2 * i + e] = j == 0 ? x : c[2 * i + e] + x;
+                    const float v = fmaf(s, p[2 * i + e], z * Q.sum[j][e]);
+                    c[2 * i + e] = j == 0 ? v : c[2 * i + e] + v;
                 }
             }
         }
@@ -224,6 +245,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         for (int m = 0; m < MT; ++m) A.a[m][0] = A.a[m][1] = A.a[m][2] = A.a[m][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < GR; ++j) A.z[j][0] = A.z[j][1] = 0.f;
+        A.inv = 0x1p127f;
     }
     static __device__ __forceinline__ void rescale(Acc& A, float f0, float f1)
     {
@@ -232,11 +254,38 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
     }
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const unsigned char* st, int span, unsigned gone, int g, int t)
+    // parameters of a span's values; gone: bit r: row r does not count
+    static __device__ __forceinline__ float load_pars(Pars& P, const unsigned char* st, int span, unsigned gone, int g)
     {
-        const unsigned char *values = st + Stage<D, true>::V + span * (8 * D), *pars = st + Stage<D, true>::VP + span * (64 * GR);
-        const uint32_t M = reg(0x00780078u), S = reg(0x41804180u);
-        uint32_t v[4][(GR + 1) / 2], vp[2][GR];
+        const unsigned char* pars = st + Stage<D, true>::VP + span * (64 * GR);
+        float top = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            get<Words>(P.p[u], pars + (rho(g) + 8 * u) * (4 * GR));
+#pragma unroll
+            for (int j = 0; j < GR; ++j) {
+                if (gone && ((gone >> (rho(g) + 8 * u)) & 1u)) P.p[u][j] = 0u;
+                top = fmaxf(top, par4_step(P.p[u][j]));
+            }
+        }
+        return top;
+    }
+    // P step stays below 2^15: weights below 2^8, step inv below 2^7.  Where a lane's largest step passes that, inv goes to where the largest of
+    // the warp has four binary places left.
+    static __device__ __forceinline__ bool too_large(const Acc& A, float top) { return top * A.inv > 128.f; }
+    static __device__ __forceinline__ void lower(Acc& A, float top)
+    {
+        top = warp_max(top);
+        if (!too_large(A, top)) return;
+        const float inv = __uint_as_float(min(257u - (__float_as_uint(top) >> 23), 254u) << 23), f = inv / A.inv;
+        A.inv = inv;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) { A.a[m][0] *= f; A.a[m][1] *= f; A.a[m][2] *= f; A.a[m][3] *= f; }
+    }
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, const unsigned char* st, int span, unsigned, int g, int t)
+    {
+        const unsigned char* values = st + Stage<D, true>::V + span * (8 * D);
+        uint32_t v[4][(GR + 1) / 2];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const Units x = *reinterpret_cast<const Units*>(values + (t + 4 * u) * (D / 2) + g * (2 * GR));   // M-rows 2t + (u & 1) + 8 (u / 2)
@@ -244,32 +293,17 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             else memcpy(v[u], &x, sizeof(x));
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) get<Words>(vp[u], pars + (rho(g) + 8 * u) * (4 * GR));
-        if (gone)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if ((gone >> (rho(g) + 8 * u)) & 1u)
-#pragma unroll
-                    for (int j = 0; j < GR; ++j) vp[u][j] = 0u;
-#pragma unroll
         for (int j = 0; j < GR; ++j) {
-            const float s0 = par4_step(vp[0][j]), s1 = par4_step(vp[1][j]);
-            const float z0 = fmaf(-16.f, s0, par4_zero(vp[0][j])), z1 = fmaf(-16.f, s1, par4_zero(vp[1][j]));
+            const float z0 = par4_zero(P.p[0][j]), z1 = par4_zero(P.p[1][j]);
             A.z[j][0] = fmaf(p[2], z1, fmaf(p[0], z0, A.z[j][0]));
             A.z[j][1] = fmaf(p[3], z1, fmaf(p[1], z0, A.z[j][1]));
-            const float x0 = p[0] * s0, x1 = p[1] * s0, x2 = p[2] * s1, x3 = p[3] * s1;
-            const uint32_t hi0 = pack_bf16(x0, x1), hi1 = pack_bf16(x2, x3);
-            const uint32_t lo0 = pack_bf16(x0 - __uint_as_float(hi0 << 16), x1 - __uint_as_float(hi0 & 0xffff0000u));
-            const uint32_t lo1 = pack_bf16(x2 - __uint_as_float(hi1 << 16), x3 - __uint_as_float(hi1 & 0xffff0000u));
-            const uint32_t h0 = movmatrix_trans(hi0), h1 = movmatrix_trans(hi1), e0 = movmatrix_trans(lo0), e1 = movmatrix_trans(lo1);
-            const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410);   // four codes of M-row 2t, of M-row 2t + 1
-            const uint32_t w = __byte_perm(v[2][j / 2], v[3][j / 2], j & 1 ? 0x7632 : 0x5410);
-            const uint32_t u0 = codes2<0>(u, M, S), u1 = codes2<1>(u, M, S), u2 = codes2<2>(u, M, S), u3 = codes2<3>(u, M, S);
-            const uint32_t w0 = codes2<0>(w, M, S), w1 = codes2<1>(w, M, S), w2 = codes2<2>(w, M, S), w3 = codes2<3>(w, M, S);
-            mma16816(A.a[2 * j], u0, u1, w0, w1, h0, h1);
-            mma16816(A.a[2 * j + 1], u2, u3, w2, w3, h0, h1);
-            mma16816(A.a[2 * j], u0, u1, w0, w1, e0, e1);
-            mma16816(A.a[2 * j + 1], u2, u3, w2, w3, e0, e1);
+            const float s0 = par4_step(P.p[0][j]) * A.inv, s1 = par4_step(P.p[1][j]) * A.inv;
+            const __half2 x0 = __floats2half2_rn(p[0] * s0, p[1] * s0), x1 = __floats2half2_rn(p[2] * s1, p[3] * s1);
+            const uint32_t h0 = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&x0)), h1 = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&x1));
+            const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410), u8 = u >> 8;   // four codes of M-row 2t, of M-row 2t + 1
+            const uint32_t w = __byte_perm(v[2][j / 2], v[3][j / 2], j & 1 ? 0x7632 : 0x5410), w8 = w >> 8;
+            mma16816_f16(A.a[2 * j], u & 0x000f000fu, u & 0x00f000f0u, w & 0x000f000fu, w & 0x00f000f0u, h0, h1);
+            mma16816_f16(A.a[2 * j + 1], u8 & 0x000f000fu, u8 & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u, h0, h1);
         }
     }
     // the groups' constant parts, summed over the lanes of a query, into the outputs
@@ -282,18 +316,16 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
                 float z = A.z[j][e];
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-                A.a[2 * j][e] += z; A.a[2 * j][2 + e] += z; A.a[2 * j + 1][e] += z; A.a[2 * j + 1][2 + e] += z;
+                const float back = 1.f / A.inv;                // (the second channel of a pair: sums of 16 c)
+#pragma unroll
+                for (int m = 2 * j; m < 2 * j + 2; ++m) {
+                    A.a[m][e] = fmaf(A.a[m][e] * LIFT, back, z);
+                    A.a[m][2 + e] = fmaf(A.a[m][2 + e] * (LIFT / 16), back, z);
+                }
             }
     }
     static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
 };
-
-__device__ StatusWord g_rows_status = LTE_STATUS_INIT;
-
-__device__ __forceinline__ void bulk_copy(uint32_t to, const unsigned char* from, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
-}
 
 template <int D, int NW, bool SWZ, bool FOUR, bool ACCUM>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
@@ -305,11 +337,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
     using St = Stage<D, FOUR>;
     constexpr int UR = St::UR, UNIT = UR / 16;
-    constexpr int SPLIT = NW == max_warps(D) ? MAX_SPLIT : 1;  // (only the largest blocks come in clusters)
-    extern __shared__ __align__(128) unsigned char s_dyn[];    // the warps' stages; [NW][most][nq] logits, behind them [NW][most] sums over passes
+    constexpr int SPLIT = clusters(D, NW) ? MAX_SPLIT : 1;
+    extern __shared__ __align__(128) unsigned char s_dyn[];    // the warps' stages; [NW][nq][most + 4] logits, behind them [NW][most + 4] sums over passes
     float* const s_log = reinterpret_cast<float*>(s_dyn + NW * St::STAGES * St::BYTES);
     auto s_acc = [&](int w, int u) { return reinterpret_cast<float*>(s_dyn + w * (St::STAGES * St::BYTES)) + u * PITCH; };
-    __shared__ __align__(8) uint64_t s_bar[NW * St::STAGES];
+    __shared__ float s_unit[MQ];
     __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
     __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
     __shared__ __align__(16) float s_ml[2][SPLIT][MQ][2];      // the cluster's shares of this block's output elements (by pass parity)
@@ -317,6 +349,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     __shared__ float s_tap[NW];
     __shared__ uint32_t s_wkey[NW];
     __shared__ int s_wpos[NW], s_wslot[NW];
+    __shared__ __align__(16) int4 s_worst[SPLIT];
     cg::cluster_group cluster = cg::this_cluster();
     const int nsplit = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int bh = blockIdx.x / nsplit, h = bh % H;
@@ -328,11 +361,6 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     const bool shared_head = SPLIT > 1 && nsplit > 1;          // (uniform in the cluster)
     if (shared_head) cluster.barrier_arrive();                 // (awaited before the first store into another block's shared memory)
     pdl_launch_dependents();
-    if (lane == 0) {
-        for (int i = 0; i < St::STAGES; ++i) tc::mbar_init(tc::smem_u32(&s_bar[wid * St::STAGES + i]), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncwarp();
     pdl_wait();
 
     // Everything whose address is known is asked for at once: the rows that a warp begins with too, whether or not they turn out to be in use.
@@ -341,38 +369,54 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     rows.total = W + R;
     const int step = NW * nsplit, first = wid * nsplit + rank;
     unsigned char* const stage = s_dyn + wid * (St::STAGES * St::BYTES);
-    const uint32_t bar = tc::smem_u32(&s_bar[wid * St::STAGES]);
-    int asked = 0, taken = 0;                                  // units of this warp, over all passes: number j goes through stage j % STAGES
-    auto ask = [&](int i) {
-        if (lane == 0) {
-            const uint32_t nr = min(UR, rows.total - UR * i), row = nr * St::ROW, par = (nr * St::PAR + 15) & ~15u;   // (a part's size in the cache is a multiple of 16)
-            const uint32_t b = bar + 8 * (asked % St::STAGES), to = tc::smem_u32(stage + (asked % St::STAGES) * St::BYTES);
-            tc::mbar_expect_tx(b, 2 * (row + par));
-            bulk_copy(to + St::K, rows.K + (size_t)i * (UR * St::ROW), row, b);
-            if (FOUR) bulk_copy(to + St::KP, rows.KP + (size_t)i * (UR * St::PAR), par, b);
-            bulk_copy(to + St::V, rows.V + (size_t)i * (UR * St::ROW), row, b);
-            if (FOUR) bulk_copy(to + St::VP, rows.VP + (size_t)i * (UR * St::PAR), par, b);
-        }
-        ++asked;
+    const uint32_t stage_at = tc::smem_u32(stage);
+    auto ask = [&](int i, int s) {                             // unit i of the head into stage s
+        const int n_rows = rows.total - UR * i;
+        const uint32_t to = stage_at + s * St::BYTES + 16 * lane;
+        const unsigned char *fk = rows.K + (size_t)i * (UR * St::ROW) + 16 * lane, *fv = rows.V + (size_t)i * (UR * St::ROW) + 16 * lane;
+        auto rows_of = [&](auto whole) {
+            constexpr int N = UR * St::ROW / 512;              // pieces of keys (of values) a lane copies
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const bool there = decltype(whole)::value || 16 * lane + 512 * u < n_rows * St::ROW;
+                if (there) tc::cp_async16(to + St::K + 512 * u, fk + 512 * u, 16);
+                if (there) tc::cp_async16(to + St::V + 512 * u, fv + 512 * u, 16);
+            }
+            if constexpr (FOUR) {                              // both parameters at once: they lie behind each other in the stage
+                constexpr int P = UR * St::PAR;                // bytes of one (the last 16 of a part of the cache are its own)
+#pragma unroll
+                for (int u = 0; u < (2 * P + 511) / 512; ++u) {
+                    const int b = 16 * lane + 512 * u, at = b < P ? b : b - P;
+                    if (b < 2 * P && (decltype(whole)::value || at < n_rows * St::PAR))
+                        tc::cp_async16(to + St::KP + 512 * u, (b < P ? rows.KP : rows.VP) + (size_t)i * P + at, 16);
+                }
+            }
+        };
+        if (n_rows >= UR) rows_of(std::true_type());
+        else rows_of(std::false_type());
     };
-    auto wait = [&](int code) { tc::mbar_wait_uni(bar + 8 * (taken % St::STAGES), (taken / St::STAGES) & 1, code, &g_rows_status); };
     auto begin = [&](int units_there) {                        // the first units of a pass
 #pragma unroll
-        for (int b = 0; b < St::STAGES; ++b)
-            if (first + b * step < units_there) ask(first + b * step);
+        for (int b = 0; b < St::STAGES; ++b) {
+            if (first + b * step < units_there) ask(first + b * step, b);
+            tc::cp_async_commit();
+        }
     };
     begin((rows.total + UR - 1) / UR);
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
     typename Gr::Query qf;
     Gr::load_q(qf, q1 + (size_t)bh * G * D, g < G, g, t);
     constexpr int PRE = NT < 256 ? 4 : 2;                      // scores and positions of the pool, before it is known whether the decision needs them
+    // A pool that the cluster's blocks would each take several rounds to look through they look through together, which costs a meeting.
+    const bool share_scan = shared_head && R > 4 * PRE * NT;
+    const int part = share_scan ? (R + nsplit - 1) / nsplit : R, pre0 = share_scan ? rank * part : 0, pre1 = min(R, pre0 + part);
     float pz[PRE];
     int pp[PRE];
 #pragma unroll
     for (int u = 0; u < PRE; ++u) {
-        const int m = tid + u * NT;
-        pz[u] = m < R ? zc[W + m] : INFINITY;
-        pp[u] = m < R ? pidx[m] : -1;
+        const int m = pre0 + tid + u * NT;
+        pz[u] = m < pre1 ? zc[W + m] : INFINITY;
+        pp[u] = m < pre1 ? pidx[m] : -1;
     }
     if (tid < D / 4) reinterpret_cast<uint4*>(s_kv)[tid] = reinterpret_cast<const uint4*>((tid < D / 8 ? k1 : v1) + (size_t)bh * D)[tid % (D / 8)];
     const int slot = n % W, p = n - W, half = rule.K / 2;
@@ -430,18 +474,39 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 
     // ---- what happens to the token leaving the window ------------------------------------------------------------
     int dst = -1, cnt_new = cnt_old;
+    bool met = false;                                          // the cluster's blocks have met already
     if (p >= 0 && R > 0 && (ACCUM || p < sink || zp > rule.zthr)) {
         if (cnt_old < R) { dst = cnt_old; cnt_new = cnt_old + 1; }
         else if (p >= sink) {
             Worst w;
 #pragma unroll
-            for (int u = 0; u < PRE; ++u) if (tid + u * NT < cnt_old) w.offer(pz[u], pp[u], tid + u * NT, sink);
-            for (int m = tid + PRE * NT; m < cnt_old; m += NT) w.offer(zc[W + m], pidx[m], m, sink);
+            for (int u = 0; u < PRE; ++u) if (pre0 + tid + u * NT < min(cnt_old, pre1)) w.offer(pz[u], pp[u], pre0 + tid + u * NT, sink);
+            constexpr int MORE = 4;                            // loads in flight
+            for (int m0 = pre0 + tid + PRE * NT; m0 < min(cnt_old, pre1); m0 += MORE * NT) {
+                float z[MORE];
+                int at[MORE];
+#pragma unroll
+                for (int u = 0; u < MORE; ++u) {
+                    const int m = min(m0 + u * NT, cnt_old - 1);   // (an entry offered twice is one)
+                    z[u] = zc[W + m]; at[u] = pidx[m];
+                }
+#pragma unroll
+                for (int u = 0; u < MORE; ++u) w.offer(z[u], at[u], min(m0 + u * NT, cnt_old - 1), sink);
+            }
             w.over_warp();
             if (NW > 1) {
                 if (lane == 0) { s_wkey[wid] = w.key; s_wpos[wid] = w.pos; s_wslot[wid] = w.slot; }
                 __syncthreads();
                 w.key = lane < NW ? s_wkey[lane] : 0xffffffffu; w.pos = lane < NW ? s_wpos[lane] : -1; w.slot = lane < NW ? s_wslot[lane] : -1;
+                w.over_warp();
+            }
+            if (share_scan) {                                  // each block has looked at its part
+                cluster.barrier_wait();                        // (every block of the cluster has started)
+                met = true;
+                if (wid == 0 && lane < nsplit) *reinterpret_cast<int4*>(cluster.map_shared_rank(&s_worst[rank], lane)) = make_int4((int)w.key, w.pos, w.slot, 0);
+                cluster.sync();
+                const int4 x = s_worst[min(lane, nsplit - 1)];
+                w.key = (uint32_t)x.x; w.pos = x.y; w.slot = x.z;
                 w.over_warp();
             }
             if (w.slot >= 0 && order_key(zp + 0.f) > w.key) dst = w.slot;
@@ -477,29 +542,33 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     };
     Move mv[MOVES];
 
-    const float scale2 = scale * 1.44269504088896340736f, jump = 8.f / scale2;   // jump: a factor of 2^8 between weights, unscaled
+    const float scale2 = scale * 1.44269504088896340736f;
     const int nqs = min(G, MQ);                                // logits kept per row
-    float* wlog = s_log + (size_t)wid * most * nqs;            // this warp's
-    float* wsum = s_log + (size_t)NW * most * nqs + (size_t)wid * most;
+    const int lpitch = most + 4;                               // (so that the queries of a store lie in different banks)
+    float* wlog = s_log + wid * lpitch * nqs;                  // this warp's
+    float* wsum = s_log + NW * lpitch * nqs + wid * lpitch;
     float fresh = 0.f;                                         // the incoming token's weights (thread 0 of the first block)
     for (int g0 = 0; g0 < G; g0 += MQ) {
         const int nq = min(MQ, G - g0);
         if (g0 > 0) {                                          // further query heads read the rows again
             Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
             __syncthreads();                                   // the previous pass's outputs, which stand in the stages, have been combined
-            tc::fence_proxy_async();
             begin(units);
         }
         typename Gr::Acc acc;
         Gr::start(acc);
+        // logits, references in units of `unit` per query; jump: a factor of 2^8 between weights
+        const float sq0 = scale2 * qf.unit[0], sq1 = scale2 * qf.unit[1], jump0 = 8.f / sq0, jump1 = 8.f / sq1;
         float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
         int kept = 0;                                          // rows whose logits this warp has kept
 
+        int at_stage = 0;
 #pragma unroll 1
         for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
-            const unsigned char* st = stage + (taken % St::STAGES) * St::BYTES;
-            wait(1);
+            const unsigned char* st = stage + at_stage * St::BYTES;
+            tc::cp_async_wait<St::STAGES - 1>();
+            __syncwarp();                                      // every lane's copies of this unit are there
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
             unsigned gone = 0;                                 // rows of the unit that do not count
@@ -513,46 +582,53 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                     if ((gone >> (16 * x + Gr::rho(g) + 8)) & 1u) c[x][2] = c[x][3] = -INFINITY;
                 }
             }
-            if constexpr (ACCUM) {                             // raw logits [row][query]
-                float* at = wlog + (size_t)(kept + Gr::rho(g)) * nq + 2 * t;
+            if constexpr (ACCUM) {                             // raw logits [query][row]
+                float* at = wlog + 2 * t * lpitch + kept + Gr::rho(g);
 #pragma unroll
                 for (int x = 0; x < UNIT; ++x) {
-                    if (2 * t < nq) { at[16 * x * nq] = c[x][0]; at[(16 * x + 8) * nq] = c[x][2]; }
-                    if (2 * t + 1 < nq) { at[16 * x * nq + 1] = c[x][1]; at[(16 * x + 8) * nq + 1] = c[x][3]; }
+                    if (2 * t < nq) { at[16 * x] = c[x][0]; at[16 * x + 8] = c[x][2]; }
+                    if (2 * t + 1 < nq) { at[lpitch + 16 * x] = c[x][1]; at[lpitch + 16 * x + 8] = c[x][3]; }
                 }
                 kept += UR;
             }
+            typename Gr::Pars vpar[UNIT];
+            float steps = 0.f;
+#pragma unroll
+            for (int x = 0; x < UNIT; ++x) steps = fmaxf(steps, Gr::load_pars(vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g));
             // The reference m follows the maximum only when that has grown by 2^8 (weights stay below 2^8, in fp32): a vote per
             // unit instead of a reduction over its rows.
             float x0 = fmaxf(c[0][0], c[0][2]), x1 = fmaxf(c[0][1], c[0][3]);
 #pragma unroll
             for (int x = 1; x < UNIT; ++x) { x0 = fmaxf(x0, fmaxf(c[x][0], c[x][2])); x1 = fmaxf(x1, fmaxf(c[x][1], c[x][3])); }
-            if (__any_sync(0xffffffffu, x0 > m0 + jump || x1 > m1 + jump)) {
-                float y0 = x0, y1 = x1;
+            if (__any_sync(0xffffffffu, fmaf(x0, Gr::LIFT, -m0) > jump0 || fmaf(x1, Gr::LIFT, -m1) > jump1 || Gr::too_large(acc, steps))) {
+                float y0 = x0 * Gr::LIFT, y1 = x1 * Gr::LIFT;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) {
                     y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, o));
                     y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, o));
                 }
                 y0 = fmaxf(y0, m0); y1 = fmaxf(y1, m1);
-                const float f0 = exp2_fast((m0 - y0) * scale2), f1 = exp2_fast((m1 - y1) * scale2);
+                const float f0 = exp2_fast((m0 - y0) * sq0), f1 = exp2_fast((m1 - y1) * sq1);
                 m0 = y0; m1 = y1;
                 l0 *= f0; l1 *= f1;
                 Gr::rescale(acc, f0, f1);
+                Gr::lower(acc, steps);
             }
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast((c[x][e] - (e & 1 ? m1 : m0)) * scale2);
+                for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast(fmaf(c[x][e], Gr::LIFT, e & 1 ? -m1 : -m0) * (e & 1 ? sq1 : sq0));
                 l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3];
             }
 #pragma unroll
-            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
-            ++taken;
+            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
             __syncwarp();                                      // every lane has read the stage
-            if (i + St::STAGES * step < units) ask(i + St::STAGES * step);
+            if (i + St::STAGES * step < units) ask(i + St::STAGES * step, at_stage);
+            tc::cp_async_commit();
+            at_stage = at_stage + 1 == St::STAGES ? 0 : at_stage + 1;
         }
-        for (; taken < asked; ++taken) wait(2);                // units asked for before it was known how many rows are in use
+        tc::cp_async_wait<0>();                                // (units asked for before it was known how many rows are in use)
+        __syncwarp();
         const bool last = g0 + MQ >= G;
         if (rank == 0 && last && dst >= 0)                     // (back by the time the write-back needs them)
 #pragma unroll
@@ -575,6 +651,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
         Gr::finish(acc);
         __syncthreads();                                       // the incoming token is there; the previous pass has been combined
+        if (wid == 0 && g == 0) { s_unit[2 * t] = qf.unit[0]; s_unit[2 * t + 1] = qf.unit[1]; }
         if (g == 0) { s_m[wid][2 * t] = m0; s_m[wid][2 * t + 1] = m1; s_l[wid][2 * t] = l0; s_l[wid][2 * t + 1] = l1; }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -592,77 +669,82 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 if (lane == 0) s_new[u] = a;
             }
         __syncthreads();
-        if (shared_head && g0 == 0) cluster.barrier_wait();    // every block of the cluster has started: its shared memory is there
+        if (shared_head && g0 == 0 && !met) cluster.barrier_wait();    // every block of the cluster has started: its shared memory is there
         const int per = nq * D / nsplit, par = (g0 / MQ) & 1;  // output elements each block of the cluster finishes
-        // reference and sum of a query over this block's rows (and the incoming token, in the first block)
-        auto block_sum = [&](int u, float& m, float& tot) {
-            m = rank == 0 ? fmaxf(s_new[u], -FLT_MAX) : -FLT_MAX;
+        // Lane u of every warp: reference and sum of query u over this block's rows (and the incoming token, in the first block)
+        auto fresh_logit = [&](int u) { return s_new[u] * (1.f / s_unit[u]); };
+        float qm = -FLT_MAX, qt = 0.f, qs = 0.f;
+        if (lane < nq) {
+            qs = scale2 * s_unit[lane];
+            if (rank == 0) qm = fmaxf(fresh_logit(lane), -FLT_MAX);
 #pragma unroll
-            for (int w2 = 0; w2 < NW; ++w2) m = fmaxf(m, s_m[w2][u]);
-            tot = rank == 0 ? exp2_fast((s_new[u] - m) * scale2) : 0.f;
+            for (int w2 = 0; w2 < NW; ++w2) qm = fmaxf(qm, s_m[w2][lane]);
+            if (rank == 0) qt = exp2_fast((fresh_logit(lane) - qm) * qs);
 #pragma unroll
-            for (int w2 = 0; w2 < NW; ++w2) tot = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_l[w2][u], tot);   // (a warp without rows: 0)
-        };
-        for (int e = tid; e < nq * D; e += NT) {
+            for (int w2 = 0; w2 < NW; ++w2) qt = fmaf(exp2_fast((s_m[w2][lane] - qm) * qs), s_l[w2][lane], qt);   // (a warp without rows: 0)
+        }
+        for (int e = tid; e < nq * D; e += NT) {               // (a warp's elements are of one query)
             const int u = e / D, ch = e - u * D;
-            float m, tot;
-            block_sum(u, m, tot);
-            float o = rank == 0 ? exp2_fast((s_new[u] - m) * scale2) * __bfloat162float(s_kv[1][ch]) : 0.f;
+            const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, qt, u), sq = __shfl_sync(0xffffffffu, qs, u);
+            float o = rank == 0 ? exp2_fast((fresh_logit(u) - m) * sq) * __bfloat162float(s_kv[1][ch]) : 0.f;
 #pragma unroll
-            for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * scale2), s_acc(w2, u)[ch], o);
+            for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * sq), s_acc(w2, u)[ch], o);
             if (!shared_head) {
                 o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
-                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * scale + logf(tot);
+                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * (scale * s_unit[u]) + logf(tot);
             } else {                                           // into the shared memory of the block that finishes this element
                 const int own = e / per;
                 *cluster.map_shared_rank(&s_in[par][rank * per + (e - own * per)], own) = o;
                 if (ch < nsplit) *reinterpret_cast<float2*>(cluster.map_shared_rank(&s_ml[par][rank][u][0], ch)) = make_float2(m, tot);
             }
         }
-        auto head_sum = [&](int u, float& m, float& tot) {     // over the whole head, once the blocks have met
-            if (!shared_head) { block_sum(u, m, tot); return; }
-            m = -FLT_MAX; tot = 0.f;
-#pragma unroll
-            for (int r2 = 0; r2 < SPLIT; ++r2) if (r2 < nsplit) m = fmaxf(m, s_ml[par][r2][u][0]);
-#pragma unroll
-            for (int r2 = 0; r2 < SPLIT; ++r2) if (r2 < nsplit) tot = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * scale2), s_ml[par][r2][u][1], tot);
-        };
         if (shared_head) {
             cluster.sync();                                    // all shares have arrived, and every row has been read
-            for (int e = tid; e < per; e += NT) {
-                const int el = rank * per + e, u = el / D, ch = el - u * D;
-                float m, tot, o = 0.f;
-                head_sum(u, m, tot);
-                for (int r2 = 0; r2 < nsplit; ++r2) o = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * scale2), s_in[par][r2 * per + e], o);
-                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
-                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * scale + logf(tot);
+            if (lane < nq) {                                   // the same over the whole head
+                qm = -FLT_MAX; qt = 0.f;
+                for (int r2 = 0; r2 < nsplit; ++r2) qm = fmaxf(qm, s_ml[par][r2][lane][0]);
+                for (int r2 = 0; r2 < nsplit; ++r2) qt = fmaf(exp2_fast((s_ml[par][r2][lane][0] - qm) * qs), s_ml[par][r2][lane][1], qt);
+            }
+            for (int e0 = wid * 32; e0 < per; e0 += NT) {
+                const int e = min(e0 + lane, per - 1), el = rank * per + e, u = el / D, ch = el - u * D;
+                const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, qt, u), sq = __shfl_sync(0xffffffffu, qs, u);
+                float o = 0.f;
+                for (int r2 = 0; r2 < nsplit; ++r2) o = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * sq), s_in[par][r2 * per + e], o);
+                if (e0 + lane < per) {
+                    o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
+                    if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * (scale * s_unit[u]) + logf(tot);
+                }
             }
         }
         if constexpr (ACCUM) {
             // ---- weights of this warp's rows into their scores.  Every block has read the old ones that its decision needs.
-            float fm = 0.f, fi = 0.f, ms[MQ], is[MQ];
-            if (lane < nq) { head_sum(lane, fm, fi); fi = 1.f / fi; }
+            const float qi = 1.f / qt;
+            for (int base = 0; base < kept; base += 32 * BATCH) {   // (the same in the whole warp)
+                const int e0 = base + lane;
+                if (last && base > 0) load_old(e0);
+                float a[BATCH] = {};
+#pragma unroll 1
+                for (int u = 0; u < nq; ++u) {
+                    const float m = __shfl_sync(0xffffffffu, qm, u), inv = __shfl_sync(0xffffffffu, qi, u), sq = __shfl_sync(0xffffffffu, qs, u);
 #pragma unroll
-            for (int u = 0; u < MQ; ++u) { ms[u] = __shfl_sync(0xffffffffu, fm, u); is[u] = __shfl_sync(0xffffffffu, fi, u); }
-            for (int e0 = lane; e0 < kept; e0 += 32 * BATCH) {
-                if (last && e0 >= 32 * BATCH) load_old(e0);
+                    for (int b = 0; b < BATCH; ++b)
+                        if (32 * b < kept - base)
+                            a[b] = fmaf(exp2_fast(fmaf(wlog[u * lpitch + min(e0 + 32 * b, kept - 1)], Gr::LIFT, -m) * sq), inv, a[b]);
+                }
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b) {
                     const int e = e0 + 32 * b, row = row_of(e);
-                    if (e >= kept) break;
-                    float a = 0.f;
-#pragma unroll
-                    for (int u = 0; u < MQ; ++u)
-                        if (u < nq) a = fmaf(exp2_fast((wlog[(size_t)e * nq + u] - ms[u]) * scale2), is[u], a);
-                    if (G > MQ) { if (g0 > 0) a += wsum[e]; wsum[e] = a; }
-                    if (last && counts(row)) zc[row == slot && p >= 0 ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old[b], a) : a;
+                    if (e >= kept) continue;
+                    if (G > MQ) { if (g0 > 0) a[b] += wsum[e]; wsum[e] = a[b]; }
+                    if (last && counts(row)) zc[row == slot && p >= 0 ? W + dst : row] = rule.decay > 0.f ? fmaf(rule.decay, old[b], a[b]) : a[b];
                 }
             }
             __syncwarp();                                      // (the next pass writes logits where these were)
-            if (rank == 0 && wid == 0)
-#pragma unroll
-                for (int u = 0; u < MQ; ++u)
-                    if (u < nq) fresh = fmaf(exp2_fast((s_new[u] - ms[u]) * scale2), is[u], fresh);
+            if (rank == 0 && wid == 0) {
+                float a = lane < nq ? exp2_fast((fresh_logit(lane) - qm) * qs) * qi : 0.f;
+                a = warp_sum(a);
+                fresh += a;
+            }
         }
     }
 
@@ -734,35 +816,56 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
 {
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
-    const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm, most_w = max_warps(p.d);
+    const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm;
     constexpr int UR = Stage<64, FOUR>::UR;                    // rows that a warp takes at a time
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
     auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
-    auto smem = [&](int nw, int split) { return (size_t)nw * most(nw * split) * kept * 4; };   // of logits
+    auto smem = [&](int nw, int split) { return (size_t)nw * (most(nw * split) + 4) * kept * 4; };   // of logits
+    // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, MEASURED.  16 heads x 1,024 rows take
+    // 7.9 us with four warps in clusters of 8, 13.1 with eight.
+    const bool is_long = rows > 4096;
+    const int most_w = p.d == 128 && !is_long ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
     int nw = 1, nsplit = 1;
     for (int c : {2, 4, 8})
         if (c <= most_w && ((BH <= n_sm * (wps / c) && rows / c >= 16) || smem(c / 2, 1) * (wps / (c / 2)) > 96 * 1024)) nw = c;
     if (nw == most_w)
-        while (nsplit < MAX_SPLIT && ((BH * nw * nsplit * 2 <= warps && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
+        while (nsplit < most_split && ((BH * nw * nsplit * 2 <= warps && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
-        if constexpr (NW <= max_warps(D)) {
+        {
             auto kern = decode_rows_mma_kernel<D, NW, decltype(s)::value, FOUR, ACCUM>;
-            static PerDeviceOnce once;
-            if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); })) return e;
             cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(BH * nsplit); cfg.blockDim = dim3(NW * 32); cfg.stream = st; cfg.dynamicSmemBytes = smem(nw, nsplit) + NW * Stage<D, FOUR>::STAGES * Stage<D, FOUR>::BYTES;
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
             attr[0].val.programmaticStreamSerializationAllowed = 1;
             attr[1].id = cudaLaunchAttributeClusterDimension;
-            attr[1].val.clusterDim.x = nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-            cfg.attrs = attr; cfg.numAttrs = nsplit > 1 ? 2 : 1;
+            attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+            constexpr size_t kMostSmem = 200 * 1024;
+            static PerDevice<int> table;                       // blocks that a cluster may have, and the kernel's limits raised
+            int split_most = 1;
+            if (int e = table.get(&split_most, [&](int* out) {
+                    if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) return cuda_status(x);
+                    *out = 8;
+                    if (!clusters(D, NW)) return (int)LTE_OK;
+                    // clusters of 16 are not portable: taken where the device can place one with the most shared memory
+                    if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) return cuda_status(x);
+                    cfg.gridDim = dim3(MAX_SPLIT); cfg.blockDim = dim3(NW * 32); cfg.dynamicSmemBytes = kMostSmem;
+                    attr[1].val.clusterDim.x = MAX_SPLIT;
+                    cfg.attrs = attr + 1; cfg.numAttrs = 1;
+                    int n = 0;
+                    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0) *out = MAX_SPLIT;
+                    else (void)cudaGetLastError();
+                    return (int)LTE_OK; })) return e;
+            const int split = nsplit < split_most ? nsplit : split_most;
+            cfg.gridDim = dim3(BH * split); cfg.blockDim = dim3(NW * 32); cfg.stream = st;
+            cfg.dynamicSmemBytes = smem(nw, split) + NW * Stage<D, FOUR>::STAGES * Stage<D, FOUR>::BYTES;
+            if (cfg.dynamicSmemBytes > kMostSmem) return (int)LTE_ERR_UNSUPPORTED;
+            attr[1].val.clusterDim.x = split;
+            cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
             return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
                                                   (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
-                                                  most(nw * nsplit)));
+                                                  most(nw * split)));
         }
-        return (int)LTE_ERR_UNSUPPORTED;
     };
     auto widths = [&](auto d, auto s) {
         switch (nw) {

@@ -18,8 +18,6 @@ int stack_bwd_tc_status_fetch_and_clear();
 int bwd_status_fetch_and_clear();
 int bwd_tail_status_fetch_and_clear();
 int decode_tc_status_fetch_and_clear();
-int decode_rows_status_fetch_and_clear();
-int decode_rows4_status_fetch_and_clear();
 
 // SM count of the current device, looked up once per device
 int device_sm_count(int* n_sm)
@@ -214,9 +212,9 @@ int lte_device_status(void)
     const int d = decode_tc_status_fetch_and_clear();
     const int t = stack_tc_status_fetch_and_clear();
     const int u = stack_bwd_tc_status_fetch_and_clear();
-    const int k = chunk_status_fetch_and_clear(), r = decode_rows_status_fetch_and_clear(), r4 = decode_rows4_status_fetch_and_clear();
-    if (h < 0 || g < 0 || f < 0 || b < 0 || bt < 0 || d < 0 || t < 0 || u < 0 || k < 0 || r < 0 || r4 < 0) return LTE_ERR_CUDA;
-    return (h == 0 && g == 0 && f == 0 && b == 0 && bt == 0 && d == 0 && t == 0 && u == 0 && k == 0 && r == 0 && r4 == 0) ? LTE_OK : LTE_ERR_DEVICE_STATUS;
+    const int k = chunk_status_fetch_and_clear();
+    if (h < 0 || g < 0 || f < 0 || b < 0 || bt < 0 || d < 0 || t < 0 || u < 0 || k < 0) return LTE_ERR_CUDA;
+    return (h == 0 && g == 0 && f == 0 && b == 0 && bt == 0 && d == 0 && t == 0 && u == 0 && k == 0) ? LTE_OK : LTE_ERR_DEVICE_STATUS;
 }
 
 size_t lte_workspace_bytes(int op, const lte_shape* s, const lte_conv* c)

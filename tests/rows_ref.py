@@ -137,8 +137,9 @@ def step(s, lay, before, q1, k1, v1, accum, decay=1.0, w=None, bias=None):
         ex = EPS * (d + 8) * ((np.abs(q[h]) @ mk.T) * scale).max(1)
         ew = 2 * ex + 2.0 ** -21 + EPS * (4 * np.maximum(0, (top - x)[wt > 1e-30].max(initial=0)) + m + 16)
         bound["lse"][h] = ex + EPS * (m + 16 + 8 * np.abs(lse[h]))
-        # (the weights of a bf16 step are multiplied as the sum of two bf16 numbers: 2^-16)
-        bound["o"][h] = ew[:, None] * (wt @ np.abs(V)) * 2 + (EPS * (m + 16) + (2.0 ** -16 if rounded else 0)) * (wt @ mv) + (2.0 ** -8 if rounded else EPS) * np.abs(o[h])
+        # (bf16 calls multiply a weight as the sum of two bf16 numbers: 2^-16 of every product; over 4 bits a weight times its row's step is
+        # rounded to fp16, 2^-12 of products with codes, w code step <= w 15 step <= w mv 15 / 48)
+        bound["o"][h] = ew[:, None] * (wt @ np.abs(V)) * 2 + (EPS * (m + 16) + (2.0 ** -12 * 15 / 48 if rounded and lay.four else 2.0 ** -16 if rounded else 0)) * (wt @ mv) + (2.0 ** -8 if rounded else EPS) * np.abs(o[h])
         if accum:
             got = wt.sum(0)
             new = {rows[r]: decay * sc[r] + got[i] if decay else got[i] for i, r in enumerate(idx)}
