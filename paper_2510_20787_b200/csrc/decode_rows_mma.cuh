@@ -427,50 +427,46 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     // word of the row's key or value codes, two runs of four weights.
     const int jsc = ACCUM ? -1 : n - half;
     constexpr int LT = D / 4, TAPS = 32 / LT;                  // lanes per tap, taps of a warp at a time
-    struct Tap { uint4 x; float w[8]; uint32_t par[2]; bool held; };
-    const int tap_word = lane % LT % (D / 8), tap_values = lane % LT / (D / 8);
-    auto tap_ask = [&](Tap& T, int tap) {
-        const int pos = n - (rule.K - 1) + tap;                // (the ring holds at least K tokens)
-        T.held = pos != n;
-        T.x = make_uint4(0, 0, 0, 0);
-        T.par[0] = T.par[1] = 0u;
+    struct Tap { uint32_t x, par[2]; float w[8]; };
+    const int tap_values = lane % LT / (D / 8), tap_word = lane % (D / 8);
+    const int tap_ch0 = tap_values ? value4_channel(tap_word, 0, GR) : key4_channel(tap_word, 0, GR);
+    const int tap_ch4 = tap_values ? value4_channel(tap_word, 4, GR) : key4_channel(tap_word, 4, GR);
+    auto tap_ask = [&](Tap& T, int tap) {                      // tap < K - 1: the token n - (K - 1) + tap, in the ring (which holds at least K)
+        const int back = slot + tap - (rule.K - 1), r = back < 0 ? back + W : back;
+        T.x = T.par[0] = T.par[1] = 0u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) T.w[e] = 0.f;
-        if (tap >= rule.K || pos < 0) return;
-        const int ch0 = tap_values ? value4_channel(tap_word, 0, GR) : key4_channel(tap_word, 0, GR);
-        const int ch4 = tap_values ? value4_channel(tap_word, 4, GR) : key4_channel(tap_word, 4, GR);
+        if (tap >= rule.K - 1 || n - (rule.K - 1) + tap < 0) return;
         const float* w = rule.w + ((size_t)h * rule.K + tap) * 2 * D + tap_values * D;
         if ((reinterpret_cast<uintptr_t>(rule.w) & 15u) == 0) {
-            const float4 a = *reinterpret_cast<const float4*>(w + ch0), b = *reinterpret_cast<const float4*>(w + ch4);
+            const float4 a = *reinterpret_cast<const float4*>(w + tap_ch0), b = *reinterpret_cast<const float4*>(w + tap_ch4);
             T.w[0] = a.x; T.w[1] = a.y; T.w[2] = a.z; T.w[3] = a.w; T.w[4] = b.x; T.w[5] = b.y; T.w[6] = b.z; T.w[7] = b.w;
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { T.w[e] = w[ch0 + e]; T.w[4 + e] = w[ch4 + e]; }
+            for (int e = 0; e < 4; ++e) { T.w[e] = w[tap_ch0 + e]; T.w[4 + e] = w[tap_ch4 + e]; }
         }
-        if (T.held) {
-            const int back = slot + tap - (rule.K - 1), r = back < 0 ? back + W : back;
-            T.x.x = reinterpret_cast<const uint32_t*>((tap_values ? rows.V : rows.K) + (size_t)r * (D / 2))[tap_word];
-            const uint32_t* par = reinterpret_cast<const uint32_t*>(tap_values ? rows.VP : rows.KP) + (size_t)r * GR;
-            T.par[0] = par[ch0 / kGroup4]; T.par[1] = par[ch4 / kGroup4];
-        } else {                                               // the incoming token, as given
-            const __nv_bfloat16* x = (tap_values ? v1 : k1) + (size_t)bh * D;
-            const uint2 a = *reinterpret_cast<const uint2*>(x + ch0), b = *reinterpret_cast<const uint2*>(x + ch4);
-            T.x = make_uint4(a.x, a.y, b.x, b.y);
-        }
+        T.x = reinterpret_cast<const uint32_t*>((tap_values ? rows.V : rows.K) + (size_t)r * (D / 2))[tap_word];
+        const uint32_t* par = reinterpret_cast<const uint32_t*>(tap_values ? rows.VP : rows.KP) + (size_t)r * GR;
+        T.par[0] = par[tap_ch0 / kGroup4]; T.par[1] = par[tap_ch4 / kGroup4];
     };
     auto tap_sum = [&](const Tap& T) {
         float a = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t u = word(T.x, e >> 1);
-            const float x = T.held ? value4((T.x.x >> (4 * e)) & 15u, T.par[e >> 2]) : __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
-            a = fmaf(T.w[e], x, a);
-        }
+        for (int e = 0; e < 8; ++e) a = fmaf(T.w[e], value4((T.x >> (4 * e)) & 15u, T.par[e >> 2]), a);
         return a;
     };
     Tap tap0;
     const bool scores = !ACCUM && rank == 0 && jsc >= 0;
-    if (scores) tap_ask(tap0, wid * TAPS + lane / LT);
+    float tap_new = 0.f;                                       // the last tap: the incoming token, as given
+    if (scores) {
+        tap_ask(tap0, wid * TAPS + lane / LT);
+        if (wid == NW - 1) {
+            const float* w = rule.w + ((size_t)h * rule.K + rule.K - 1) * 2 * D;
+#pragma unroll
+            for (int c = 0; c < CPL; ++c)
+                tap_new += w[lane + 32 * c] * __bfloat162float(k1[(size_t)bh * D + lane + 32 * c]) + w[D + lane + 32 * c] * __bfloat162float(v1[(size_t)bh * D + lane + 32 * c]);
+        }
+    }
 
     // ---- what happens to the token leaving the window ------------------------------------------------------------
     int dst = -1, cnt_new = cnt_old;
@@ -516,13 +512,40 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     const int masked_pool = dst >= 0 && dst < cnt_old ? W + dst : -32;   // ... and then the entry it replaces does not
 
     if (scores) {
-        float a = tap_sum(tap0);
-        for (int tap = (wid + NW) * TAPS; tap < rule.K; tap += NW * TAPS) {
+        float a = tap_new + tap_sum(tap0);
+        for (int tap = (wid + NW) * TAPS; tap < rule.K - 1; tap += NW * TAPS) {
             tap_ask(tap0, tap + lane / LT);
             a += tap_sum(tap0);
         }
         a = warp_sum(a);
         if (lane == 0) s_tap[wid] = a;
+    }
+
+    // 4 bits: the incoming row's codes, in the last warp of the first block, while the first rows are on their way: eight channels a lane, four
+    // lanes a group
+    const int new_piece = min(lane, D / 4 - 1) % (D / 8);
+    const bool new_values = min(lane, D / 4 - 1) >= D / 8;
+    uint32_t new_codes = 0u, new_par = 0u;
+    if constexpr (FOUR) {
+        if (rank == 0 && wid == NW - 1) {
+            const uint4 u = reinterpret_cast<const uint4*>((new_values ? v1 : k1) + (size_t)bh * D)[new_piece];
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(word(u, i) << 16); f[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
+            float lo = f[0], hi = f[0];
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+                bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+            }
+            new_par = group4(lo, hi, bad);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) new_codes |= code4(f[i], new_par) << (4 * i);
+        }
     }
 
     // the popped row's words, read before the slot is written: thread e of the last ones moves word e
@@ -555,6 +578,16 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             __syncthreads();                                   // the previous pass's outputs, which stand in the stages, have been combined
             begin(units);
         }
+        if (rank == 0)                                         // the incoming token's logits
+            for (int u = wid; u < nq; u += NW) {
+                float a = 0.f;
+#pragma unroll
+                for (int c = 0; c < CPL; ++c)
+                    a = fmaf(__bfloat162float(q1[((size_t)bh * G + g0 + u) * D + lane + 32 * c]), __bfloat162float(k1[(size_t)bh * D + lane + 32 * c]), a);
+                a = warp_sum(a);
+                const float unit = __shfl_sync(0xffffffffu, u & 1 ? qf.unit[1] : qf.unit[0], u >> 1);
+                if (lane == 0) s_new[u] = a * __uint_as_float((254u << 23) - __float_as_uint(unit));   // (the inverse of a power of two)
+            }
         typename Gr::Acc acc;
         Gr::start(acc);
         // logits, references in units of `unit` per query; jump: a factor of 2^8 between weights
@@ -659,39 +692,30 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             if (2 * t < nq) *reinterpret_cast<float2*>(&s_acc(wid, 2 * t)[ch]) = make_float2(acc.a[i][0], acc.a[i][2]);
             if (2 * t + 1 < nq) *reinterpret_cast<float2*>(&s_acc(wid, 2 * t + 1)[ch]) = make_float2(acc.a[i][1], acc.a[i][3]);
         }
-        if (rank == 0)                                         // the incoming token's logits
-            for (int u = wid; u < nq; u += NW) {
-                float a = 0.f;
-#pragma unroll
-                for (int c = 0; c < CPL; ++c)
-                    a = fmaf(__bfloat162float(q1[((size_t)bh * G + g0 + u) * D + lane + 32 * c]), __bfloat162float(s_kv[0][lane + 32 * c]), a);
-                a = warp_sum(a);
-                if (lane == 0) s_new[u] = a;
-            }
         __syncthreads();
         if (shared_head && g0 == 0 && !met) cluster.barrier_wait();    // every block of the cluster has started: its shared memory is there
         const int per = nq * D / nsplit, par = (g0 / MQ) & 1;  // output elements each block of the cluster finishes
         // Lane u of every warp: reference and sum of query u over this block's rows (and the incoming token, in the first block)
-        auto fresh_logit = [&](int u) { return s_new[u] * (1.f / s_unit[u]); };
         float qm = -FLT_MAX, qt = 0.f, qs = 0.f;
         if (lane < nq) {
             qs = scale2 * s_unit[lane];
-            if (rank == 0) qm = fmaxf(fresh_logit(lane), -FLT_MAX);
+            if (rank == 0) qm = fmaxf(s_new[lane], -FLT_MAX);
 #pragma unroll
             for (int w2 = 0; w2 < NW; ++w2) qm = fmaxf(qm, s_m[w2][lane]);
-            if (rank == 0) qt = exp2_fast((fresh_logit(lane) - qm) * qs);
+            if (rank == 0) qt = exp2_fast((s_new[lane] - qm) * qs);
 #pragma unroll
             for (int w2 = 0; w2 < NW; ++w2) qt = fmaf(exp2_fast((s_m[w2][lane] - qm) * qs), s_l[w2][lane], qt);   // (a warp without rows: 0)
         }
+        float qi = 1.f / qt;
+        if (!shared_head && wid == 0 && lane < nq) lse1[(size_t)bh * G + g0 + lane] = qm * (scale * s_unit[lane]) + logf(qt);
         for (int e = tid; e < nq * D; e += NT) {               // (a warp's elements are of one query)
             const int u = e / D, ch = e - u * D;
-            const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, qt, u), sq = __shfl_sync(0xffffffffu, qs, u);
-            float o = rank == 0 ? exp2_fast((fresh_logit(u) - m) * sq) * __bfloat162float(s_kv[1][ch]) : 0.f;
+            const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, shared_head ? qt : qi, u), sq = __shfl_sync(0xffffffffu, qs, u);
+            float o = rank == 0 ? exp2_fast((s_new[u] - m) * sq) * __bfloat162float(s_kv[1][ch]) : 0.f;
 #pragma unroll
             for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * sq), s_acc(w2, u)[ch], o);
             if (!shared_head) {
-                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
-                if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * (scale * s_unit[u]) + logf(tot);
+                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * tot);
             } else {                                           // into the shared memory of the block that finishes this element
                 const int own = e / per;
                 *cluster.map_shared_rank(&s_in[par][rank * per + (e - own * per)], own) = o;
@@ -705,20 +729,18 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 for (int r2 = 0; r2 < nsplit; ++r2) qm = fmaxf(qm, s_ml[par][r2][lane][0]);
                 for (int r2 = 0; r2 < nsplit; ++r2) qt = fmaf(exp2_fast((s_ml[par][r2][lane][0] - qm) * qs), s_ml[par][r2][lane][1], qt);
             }
+            qi = 1.f / qt;
+            if (rank == 0 && wid == 0 && lane < nq) lse1[(size_t)bh * G + g0 + lane] = qm * (scale * s_unit[lane]) + logf(qt);
             for (int e0 = wid * 32; e0 < per; e0 += NT) {
                 const int e = min(e0 + lane, per - 1), el = rank * per + e, u = el / D, ch = el - u * D;
-                const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, qt, u), sq = __shfl_sync(0xffffffffu, qs, u);
+                const float m = __shfl_sync(0xffffffffu, qm, u), inv = __shfl_sync(0xffffffffu, qi, u), sq = __shfl_sync(0xffffffffu, qs, u);
                 float o = 0.f;
                 for (int r2 = 0; r2 < nsplit; ++r2) o = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * sq), s_in[par][r2 * per + e], o);
-                if (e0 + lane < per) {
-                    o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o / tot);
-                    if (ch == 0) lse1[(size_t)bh * G + g0 + u] = m * (scale * s_unit[u]) + logf(tot);
-                }
+                if (e0 + lane < per) o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * inv);
             }
         }
         if constexpr (ACCUM) {
             // ---- weights of this warp's rows into their scores.  Every block has read the old ones that its decision needs.
-            const float qi = 1.f / qt;
             for (int base = 0; base < kept; base += 32 * BATCH) {   // (the same in the whole warp)
                 const int e0 = base + lane;
                 if (last && base > 0) load_old(e0);
@@ -741,7 +763,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             }
             __syncwarp();                                      // (the next pass writes logits where these were)
             if (rank == 0 && wid == 0) {
-                float a = lane < nq ? exp2_fast((fresh_logit(lane) - qm) * qs) * qi : 0.f;
+                float a = lane < nq ? exp2_fast((s_new[lane] - qm) * qs) * qi : 0.f;
                 a = warp_sum(a);
                 fresh += a;
             }
@@ -755,38 +777,16 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         for (int u = 0; u < MOVES; ++u)
             if (NT - 1 - tid + u * NT < WORDS) *place(NT - 1 - tid + u * NT, W + dst) = mv[u];
     if constexpr (FOUR) {
-        // the incoming row's codes: eight channels a lane, four lanes a group
-        if (wid == NW - 1) {
-            const int e = min(lane, D / 4 - 1), piece = e % (D / 8), grp = piece / 4, tt = piece % 4;
-            const bool values = e >= D / 8;
-            const uint4 u = reinterpret_cast<const uint4*>(s_kv[values])[piece];
-            float f[8], lo, hi;
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(word(u, i) << 16); f[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
-            lo = hi = f[0];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+        if (wid == NW - 1 && lane < D / 4) {
+            unsigned char* codes = blk + (new_values ? L.off_v : L.off_k) + (size_t)slot * (D / 2);
+            const int grp = new_piece / 4, tt = new_piece % 4;
+            if (new_values) {
+                reinterpret_cast<uint16_t*>(codes)[2 * tt * GR + grp] = (uint16_t)new_codes;
+                reinterpret_cast<uint16_t*>(codes)[(2 * tt + 1) * GR + grp] = (uint16_t)(new_codes >> 16);
+            } else {
+                reinterpret_cast<uint32_t*>(codes)[tt * GR + grp] = new_codes;
             }
-            const uint32_t par = group4(lo, hi, bad);
-            uint32_t w = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w |= code4(f[i], par) << (4 * i);
-            if (lane < D / 4) {
-                unsigned char* codes = blk + (values ? L.off_v : L.off_k) + (size_t)slot * (D / 2);
-                if (values) {
-                    reinterpret_cast<uint16_t*>(codes)[2 * tt * GR + grp] = (uint16_t)w;
-                    reinterpret_cast<uint16_t*>(codes)[(2 * tt + 1) * GR + grp] = (uint16_t)(w >> 16);
-                } else {
-                    reinterpret_cast<uint32_t*>(codes)[tt * GR + grp] = w;
-                }
-                if (tt == 0) reinterpret_cast<uint32_t*>(blk + (values ? L.off_vp : L.off_kp))[(size_t)slot * GR + grp] = par;
-            }
+            if (tt == 0) reinterpret_cast<uint32_t*>(blk + (new_values ? L.off_vp : L.off_kp))[(size_t)slot * GR + grp] = new_par;
         }
     } else {
         for (int e = tid; e < WORDS; e += NT) *reinterpret_cast<uint4*>(place(e, slot)) = reinterpret_cast<const uint4*>(s_kv)[e];
