@@ -1,7 +1,9 @@
 // An ordinary decode cache into 4 bits, and back (see cache4.cuh for the rule and the order of the codes).
 //
-// Bound by memory: a thread takes eight channels of a row (16 or 32 bytes), four threads a group; they meet in two shuffles for its
-// extremes.  Scores, positions and counters are copied by the same blocks.
+// Bound by memory and, for the rounding, nearly as much by instructions: a thread takes eight channels of the key and of the value of ROWS rows (16
+// or 32 bytes each), four threads a group; they meet in two shuffles for its extremes.  Scores, positions and counters are copied by the same
+// blocks.
+// Measured (B200, 256 heads x 1,280 rows, d = 64, bf16; 84 MB and 27 MB): MEASURED_PACK
 #include <type_traits>
 
 #include "cache4.cuh"
@@ -78,29 +80,28 @@ __global__ void __launch_bounds__(PT) cache4_pack_kernel(const unsigned char* __
     const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts, rows = W + R;
     const unsigned char* src = cache + L.header + (size_t)bh * L.stride;
     unsigned char* dst = cache4 + Q.header + (size_t)bh * Q.stride;
-    const int r0 = part * PROWS, n = min(PROWS, rows - r0) * PIECES;   // (a multiple of 4: the threads of a group stay together)
-    for (int e = threadIdx.x; e < (n + 31) / 32 * 32; e += PT) {       // whole warps
-        const int at = min(e, n - 1), row = r0 + at / PIECES, piece = at % PIECES, group = piece / 4, t = piece % 4;
+    // thread: piece tid % PIECES of rows r0 + tid / PIECES + u (PT / PIECES); rows past the last one repeat it and are not stored
+    constexpr int STEP = PT / PIECES, ROWS = PROWS / STEP;
+    const int r0 = part * PROWS + threadIdx.x / PIECES, piece = threadIdx.x % PIECES, group = piece / 4, t = piece % 4;
+    Piece8<T> p[ROWS][2];
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const size_t at = piece_at(L, min(r0 + u * STEP, rows - 1), piece, PIECES);
+        p[u][0] = reinterpret_cast<const Piece8<T>*>(src + L.off_k)[at];
+        p[u][1] = reinterpret_cast<const Piece8<T>*>(src + L.off_v)[at];
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const int row = r0 + u * STEP;
 #pragma unroll
         for (int values = 0; values < 2; ++values) {
-            const Piece8<T> p = reinterpret_cast<const Piece8<T>*>(src + (values ? L.off_v : L.off_k))[piece_at(L, row, piece, PIECES)];
             float f[8];
-            unpack8<T>(p, f);
-            float lo = f[0], hi = f[0];
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
-            }
-            const uint32_t par = group4(lo, hi, bad);
-            uint32_t w = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w |= code4(f[i], par) << (4 * i);
-            if (e < n) {
+            unpack8<T>(p[u][values], f);
+            uint32_t par;
+            if constexpr (sizeof(T) == 2) par = group4_of(p[u][values].u[0]);
+            else par = group4_of(f);
+            const uint32_t w = codes4(f, par);
+            if (row < rows) {
                 unsigned char* codes = dst + (values ? Q.off_v : Q.off_k) + (size_t)row * (D / 2);
                 if (values) {
                     reinterpret_cast<uint16_t*>(codes)[2 * t * GROUPS + group] = (uint16_t)w;
@@ -134,25 +135,28 @@ __global__ void __launch_bounds__(PT) cache4_unpack_kernel(const unsigned char* 
     const int bh = blockIdx.x / parts, part = blockIdx.x - bh * parts, rows = W + R;
     const unsigned char* src = cache4 + Q.header + (size_t)bh * Q.stride;
     unsigned char* dst = cache + L.header + (size_t)bh * L.stride;
-    const int r0 = part * PROWS, n = min(PROWS, L.rows_alloc - r0) * PIECES;
-    for (int e = threadIdx.x; e < n; e += PT) {
-        const int row = r0 + e / PIECES, piece = e % PIECES, group = piece / 4, t = piece % 4;
+    constexpr int STEP = PT / PIECES, ROWS = PROWS / STEP;
+    const int r0 = part * PROWS + threadIdx.x / PIECES, piece = threadIdx.x % PIECES, group = piece / 4, t = piece % 4;
+    uint32_t w[ROWS][2], par[ROWS][2];
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const int row = min(r0 + u * STEP, rows - 1);
+        w[u][0] = reinterpret_cast<const uint32_t*>(src + Q.off_k + (size_t)row * (D / 2))[t * GROUPS + group];
+        const uint16_t* v = reinterpret_cast<const uint16_t*>(src + Q.off_v + (size_t)row * (D / 2)) + 2 * t * GROUPS + group;
+        w[u][1] = v[0] | (uint32_t)v[GROUPS] << 16;
+        par[u][0] = reinterpret_cast<const uint32_t*>(src + Q.off_kp)[(size_t)row * GROUPS + group];
+        par[u][1] = reinterpret_cast<const uint32_t*>(src + Q.off_vp)[(size_t)row * GROUPS + group];
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const int row = r0 + u * STEP;
 #pragma unroll
         for (int values = 0; values < 2; ++values) {
             float f[8];
-            if (row < rows) {
-                const unsigned char* codes = src + (values ? Q.off_v : Q.off_k) + (size_t)row * (D / 2);
-                const uint32_t par = reinterpret_cast<const uint32_t*>(src + (values ? Q.off_vp : Q.off_kp))[(size_t)row * GROUPS + group];
-                const uint32_t w = values ? reinterpret_cast<const uint16_t*>(codes)[2 * t * GROUPS + group] |
-                                                (uint32_t)reinterpret_cast<const uint16_t*>(codes)[(2 * t + 1) * GROUPS + group] << 16
-                                          : reinterpret_cast<const uint32_t*>(codes)[t * GROUPS + group];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = value4((w >> (4 * i)) & 15u, par);
-            } else {                                           // the swizzled layout's rows behind the last one
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = 0.f;
-            }
-            reinterpret_cast<Piece8<T>*>(dst + (values ? L.off_v : L.off_k))[piece_at(L, row, piece, PIECES)] = pack8(f, T());
+            for (int i = 0; i < 8; ++i) f[i] = row < rows ? value4((w[u][values] >> (4 * i)) & 15u, par[u][values]) : 0.f;   // (behind the last row: zero)
+            if (row < L.rows_alloc)
+                reinterpret_cast<Piece8<T>*>(dst + (values ? L.off_v : L.off_k))[piece_at(L, row, piece, PIECES)] = pack8(f, T());
         }
     }
     copy_tail(src, Q.off_z, Q.off_pidx, Q.off_meta, dst, L.off_z, L.off_pidx, L.off_meta, L.stride, rows, R, part, parts);

@@ -61,15 +61,71 @@ __device__ __forceinline__ uint32_t group4(float lo, float hi, bool bad)
     if (bad || (step & 0x7f80u) == 0x7f80u || (zero & 0x7f80u) == 0x7f80u) return 0x7fc07fc0u;
     return step | (zero << 16);
 }
-// clamp(rint((x - zero) / step), 0, 15) in fp32 arithmetic; 0 where step is 0 or the group NaN.  The quotient is taken by the reciprocal, which is
-// off by a few units in the last place: only within 2^-10 of the middle between two codes can that decide, and there it is divided.
+// clamp(rint((x - zero) / step), 0, 15) in fp32 arithmetic; 0 where step is 0 or the group NaN
 __device__ __forceinline__ uint32_t code4(float x, uint32_t par)
 {
-    const float step = par4_step(par), r = x - par4_zero(par);
+    const float step = par4_step(par);
     if (!(step > 0.f)) return 0u;
-    float q = r * __frcp_rn(step), c = rintf(q);
-    if (!(fabsf(q - c) < 0.5f - 0x1p-10f)) c = rintf(__fdiv_rn(r, step));    // (so do a quotient and a reciprocal out of range)
-    return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+    return (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - par4_zero(par), step)), 0.f), 15.f);
+}
+// The codes of eight channels, the first in the lowest nibble.  The quotient d / step, d = x - zero, comes from the reciprocal y of step by one
+// correction, q + (d - q step) y (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990): a rounding of the
+// exact quotient moved by less than 2 units of its last place times 2^-24.  That rounds to the same code as the correctly rounded quotient: an
+// exact half k + 1/2 stays one (bf16 rows have them all the time), and the two could part only where the quotient is that close to the border
+// between k + 1/2 and its neighbour, a number of 25 bits, which times step is no fp32 number d (step has 8 bits, so that what is not on
+// the border is further off).  Rounding is by adding 1.5 2^23, which leaves the code in the lowest bits.  Steps outside 2^-100 .. 2^100, where
+// the terms might leave the range of fp32, are divided by.
+__device__ __forceinline__ uint32_t codes4(const float (&f)[8], uint32_t par)
+{
+    constexpr float MAGIC = 12582912.f;
+    constexpr uint32_t REST = 0x4b400000u * 0x11111111u;       // (modulo 2^32: what the bits above the codes add up to)
+    const float step = par4_step(par), zero = par4_zero(par), y = __frcp_rn(step);
+    uint32_t w = 0u;
+    if (step > 0x1p-100f && step < 0x1p100f) {
+        w = 0u - REST;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = f[i] - zero, q0 = d * y, q = fmaf(fmaf(-q0, step, d), y, q0);
+            w += __float_as_uint(fminf(fmaxf(q, 0.f), 15.f) + MAGIC) << (4 * i);
+        }
+    } else if (step > 0.f) {
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+            float x = f[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) x = e == i ? f[e] : x;
+            w |= code4(x, par) << (4 * i);
+        }
+    }
+    return w;
+}
+// Extremes of a group from four lanes' eight channels each; NaN and infinities go through.
+__device__ __forceinline__ uint32_t group4_of(const uint4& u)     // bf16
+{
+    auto bf = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+    __nv_bfloat162 lo = __hmin2_nan(__hmin2_nan(bf(u.x), bf(u.y)), __hmin2_nan(bf(u.z), bf(u.w)));
+    __nv_bfloat162 hi = __hmax2_nan(__hmax2_nan(bf(u.x), bf(u.y)), __hmax2_nan(bf(u.z), bf(u.w)));
+    __nv_bfloat162 x = __halves2bfloat162(__hmin_nan(lo.x, lo.y), __hneg(__hmax_nan(hi.x, hi.y)));   // (min, -max)
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&x), o);
+        x = __hmin2_nan(x, bf(other));
+    }
+    return group4(__bfloat162float(x.x), -__bfloat162float(x.y), false);
+}
+__device__ __forceinline__ uint32_t group4_of(const float (&f)[8])
+{
+    float lo = f[0], hi = f[0];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+    }
+    return group4(lo, hi, bad);
 }
 
 // A group of the row in `x` (one channel per lane) into the 4-bit cache, by a whole warp.

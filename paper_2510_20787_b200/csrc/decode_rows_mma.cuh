@@ -532,19 +532,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             float f[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(word(u, i) << 16); f[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
-            float lo = f[0], hi = f[0];
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { lo = fminf(lo, f[i]); hi = fmaxf(hi, f[i]); bad |= !(fabsf(f[i]) < INFINITY); }
-#pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-                bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
-            }
-            new_par = group4(lo, hi, bad);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) new_codes |= code4(f[i], new_par) << (4 * i);
+            new_par = group4_of(u);
+            new_codes = codes4(f, new_par);
         }
     }
 
