@@ -1,8 +1,12 @@
-// Decode step (lte_attn_decode_accum, lte_attn_decode4, lte_attn_decode4_accum) on the fp32 ALUs.
+// Decode step (lte_attn_decode_accum, lte_attn_decode4, lte_attn_decode4_accum) for fp32 calls, on the fp32 ALUs.
 //
 // A block of 256 threads a head, or a cluster of up to eight that share its rows where heads are few.  Pool decision, logits of the block's
 // rows into shared memory, softmax over them, weighted values; the blocks then meet through distributed shared memory, and each adds
 // the weights of its rows to their scores: the weights need the sum over all rows, so the logits stay until then.
+// A row is shared by the LPR lanes that hold its 16-byte pieces (4 bits: its 4-byte words).  What bounds it is the latency of its loads and the sums over
+// those lanes: a thread has BATCH rows in flight, and their partial sums for all query heads are added up together, half of them handed to
+// the other half of the lanes in every round (15 shuffles in the place of 64 for four rows, four query heads and 16 lanes).
+// Measured (B200, a step in a CUDA graph): MEASURED_F32
 #include <cfloat>
 #include <cooperative_groups.h>
 
@@ -15,44 +19,71 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int DT = 256;
-constexpr int QP = 4;                                          // query heads per pass
+constexpr int BATCH = 4;                                       // rows a thread has in flight
 constexpr int MAX_SPLIT = 8;
 
 // How a lane sees a row: LPR lanes of E channels each.
-template <typename T, int D, bool FOUR> struct Held {
-    static constexpr int E = FOUR ? 8 : 16 / (int)sizeof(T), LPR = D / E, GROUPS = D / kGroup4;
+template <int D, bool FOUR> struct Held {
+    static constexpr int E = FOUR ? 8 : 4, LPR = D / E, GROUPS = D / kGroup4;
+    struct Raw { uint4 u; };                                   // four channels, or a word of codes and its two parameters
     static __device__ __forceinline__ int channel(bool values, int seg, int e)
     {
         return !FOUR ? seg * E + e : values ? value4_channel(seg, e, GROUPS) : key4_channel(seg, e, GROUPS);
     }
-    static __device__ __forceinline__ void load(const unsigned char* rows, const unsigned char* par, const CacheLayout& C, bool values, int row, int seg,
-                                                float (&f)[E])
+    static __device__ __forceinline__ Raw load(const unsigned char* rows, const unsigned char* par, bool values, int row, int seg)
+    {
+        Raw r;
+        if constexpr (FOUR) {
+            r.u.x = reinterpret_cast<const uint32_t*>(rows)[(size_t)row * LPR + seg];
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(par) + (size_t)row * GROUPS;
+            r.u.y = p[channel(values, seg, 0) / kGroup4]; r.u.z = p[channel(values, seg, 4) / kGroup4];
+        } else {
+            r.u = reinterpret_cast<const uint4*>(rows)[(size_t)row * LPR + seg];
+        }
+        return r;
+    }
+    static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[E])
     {
         if constexpr (FOUR) {
-            const uint32_t w = reinterpret_cast<const uint32_t*>(rows)[(size_t)row * LPR + seg];
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(par) + (size_t)row * GROUPS;
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = value4((w >> (4 * e)) & 15u, p[channel(values, seg, e) / kGroup4]);
+            for (int e = 0; e < E; ++e) f[e] = value4((r.u.x >> (4 * e)) & 15u, e < 4 ? r.u.y : r.u.z);
         } else {
-            const int at = sizeof(T) == 2 ? cache_chunk_pos(C, row, seg) : seg;
-            const uint4 u = reinterpret_cast<const uint4*>(rows)[(size_t)row * LPR + at];
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 2) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-                else f[i] = __uint_as_float(w[i]);
-            }
+            f[0] = __uint_as_float(r.u.x); f[1] = __uint_as_float(r.u.y); f[2] = __uint_as_float(r.u.z); f[3] = __uint_as_float(r.u.w);
         }
     }
 };
 
-template <typename T, int D, bool FOUR, bool ACCUM>
-__global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restrict__ cache, RowsLayout L, CacheLayout C, const T* __restrict__ q1,
-                                                         const T* __restrict__ k1, const T* __restrict__ v1, T* __restrict__ o1,
+// V values per lane, summed over the L lanes that share `seg` (0 .. L - 1): afterwards lane seg has, in x[0 .. max(V / L, 1) - 1], the sums of the values
+// from index (seg's bits, the lowest first, as halves of V) on; `first` is that index.
+template <int V, int L> __device__ __forceinline__ int sum_lanes(float (&x)[V], int seg)
+{
+    int first = 0, n = V;
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) {
+        if (n > 1) {
+            n >>= 1;
+            const bool up = seg & o;
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i)
+                if (i < n) {
+                    const float give = up ? x[i] : x[i + n], keep = up ? x[i + n] : x[i];
+                    x[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                }
+            first += up ? n : 0;
+        } else {
+            x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+        }
+    }
+    return first;
+}
+
+template <int D, int QP, bool FOUR, bool ACCUM>                // QP: query heads per pass
+__global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restrict__ cache, RowsLayout L, const float* __restrict__ q1,
+                                                         const float* __restrict__ k1, const float* __restrict__ v1, float* __restrict__ o1,
                                                          float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink, float scale, int G,
                                                          int most)                       // most: rows a block may have
 {
-    using Row = Held<T, D, FOUR>;
+    using Row = Held<D, FOUR>;
     constexpr int E = Row::E, LPR = Row::LPR, RPP = DT / LPR, NW = DT / 32;
     extern __shared__ __align__(16) float s_log[];             // [most][nq] logits, then weights; behind them [most] sums over passes
     __shared__ float s_q[QP][D], s_kn[D], s_vn[D];
@@ -72,7 +103,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
     pdl_wait();
 
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R), slot = n % W, p = n - W;
-    for (int c = tid; c < D; c += DT) { s_kn[c] = to_f<T>(k1[(size_t)bh * D + c]); s_vn[c] = to_f<T>(v1[(size_t)bh * D + c]); }
+    for (int c = tid; c < D; c += DT) { s_kn[c] = k1[(size_t)bh * D + c]; s_vn[c] = v1[(size_t)bh * D + c]; }
 
     // ---- what happens to the token leaving the window (every block of the cluster finds the same) ------------------
     const float zp = p >= 0 ? zc[slot] : 0.f;
@@ -103,7 +134,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
     for (int g0 = 0; g0 < G; g0 += QP) {
         const int nq = min(QP, G - g0);
         __syncthreads();
-        for (int c = tid; c < QP * D; c += DT) s_q[c / D][c % D] = c / D < nq ? to_f<T>(q1[((size_t)bh * G + g0) * D + c]) : 0.f;
+        for (int c = tid; c < QP * D; c += DT) s_q[c / D][c % D] = c / D < nq ? q1[((size_t)bh * G + g0) * D + c] : 0.f;
         __syncthreads();
         // ---- logits -----------------------------------------------------------------------------------------------
         {
@@ -112,20 +143,35 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
             for (int u = 0; u < QP; ++u)
 #pragma unroll
                 for (int e = 0; e < E; ++e) qf[u][e] = s_q[u][Row::channel(false, seg, e)];
-            for (int r0 = 0; r0 < mine; r0 += RPP) {
-                const int u = r0 + rsub, row = row_of(min(u, mine - 1));
-                float kf[E], x[QP];
-                Row::load(blk + L.off_k, blk + L.off_kp, C, false, row, seg, kf);
+            // value r * QP + g of a lane: row r of the batch, query head g
+            typename Row::Raw raw[BATCH];
+            auto ask = [&](int r0) {
 #pragma unroll
-                for (int g = 0; g < QP; ++g) {
-                    x[g] = 0.f;
+                for (int r = 0; r < BATCH; ++r) raw[r] = Row::load(blk + L.off_k, blk + L.off_kp, false, row_of(min(r0 + r * RPP + rsub, mine - 1)), seg);
+            };
+            if (mine > 0) ask(0);
+            for (int r0 = 0; r0 < mine; r0 += BATCH * RPP) {
+                float x[BATCH * QP];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) x[g] = fmaf(qf[g][e], kf[e], x[g]);
+                for (int r = 0; r < BATCH; ++r) {
+                    float kf[E];
+                    Row::unpack(raw[r], kf);
 #pragma unroll
-                    for (int o = LPR / 2; o > 0; o >>= 1) x[g] += __shfl_xor_sync(0xffffffffu, x[g], o);
+                    for (int g = 0; g < QP; ++g) {
+                        x[r * QP + g] = 0.f;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[r * QP + g] = fmaf(qf[g][e], kf[e], x[r * QP + g]);
+                    }
                 }
-                if (seg == 0 && u < mine)
-                    for (int g = 0; g < nq; ++g) s_log[u * nq + g] = seen(row) ? x[g] * scale : -INFINITY;
+                if (r0 + BATCH * RPP < mine) ask(r0 + BATCH * RPP);
+                const int at = sum_lanes<BATCH * QP, LPR>(x, seg);
+                constexpr int LEFT = BATCH * QP > LPR ? BATCH * QP / LPR : 1;   // sums a lane is left with (some lanes have the same one)
+                if (BATCH * QP >= LPR || seg < BATCH * QP)
+#pragma unroll
+                    for (int i = 0; i < LEFT; ++i) {
+                        const int u = r0 + (at + i) / QP * RPP + rsub, g = (at + i) % QP;
+                        if (u < mine && g < nq) s_log[u * nq + g] = seen(row_of(u)) ? x[i] * scale : -INFINITY;
+                    }
             }
         }
         if (wid < nq) {                                        // the incoming token's
@@ -171,16 +217,28 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
             for (int g = 0; g < QP; ++g)
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[g][e] = 0.f;
-            for (int u = rsub; u < mine; u += RPP) {
-                const int row = row_of(u);
-                if (!seen(row)) continue;
-                float vf[E];
-                Row::load(blk + L.off_v, blk + L.off_vp, C, true, row, seg, vf);
+            typename Row::Raw raw[BATCH];
+            auto ask = [&](int r0) {
 #pragma unroll
-                for (int g = 0; g < QP; ++g) {
-                    const float w = g < nq ? s_log[u * nq + g] : 0.f;
+                for (int r = 0; r < BATCH; ++r) raw[r] = Row::load(blk + L.off_v, blk + L.off_vp, true, row_of(min(r0 + r * RPP + rsub, mine - 1)), seg);
+            };
+            if (mine > 0) ask(0);
+            for (int r0 = 0; r0 < mine; r0 += BATCH * RPP) {
+                float vf[BATCH][E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) acc[g][e] = g < nq ? fmaf(w, vf[e], acc[g][e]) : 0.f;
+                for (int r = 0; r < BATCH; ++r) Row::unpack(raw[r], vf[r]);
+                if (r0 + BATCH * RPP < mine) ask(r0 + BATCH * RPP);
+#pragma unroll
+                for (int r = 0; r < BATCH; ++r) {
+                    const int u = r0 + r * RPP + rsub;
+                    if (u >= mine || !seen(row_of(u))) continue;   // (zero times an infinite value is NaN)
+#pragma unroll
+                    for (int g = 0; g < QP; ++g)
+                        if (g < nq) {
+                            const float w = s_log[u * nq + g];
+#pragma unroll
+                            for (int e = 0; e < E; ++e) acc[g][e] = fmaf(w, vf[r][e], acc[g][e]);
+                        }
                 }
             }
 #pragma unroll
@@ -223,7 +281,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
             for (int g2 = 0; g2 < QP; ++g2) if (g2 == g) { m = top[g2]; l = tot[g2]; }
             float o = 0.f;
             for (int r = 0; r < nsplit; ++r) o += __expf(*cluster.map_shared_rank(&s_m[g], r) - m) * *cluster.map_shared_rank(&s_o[g][c], r);
-            o1[((size_t)bh * G + g0) * D + e] = from_f<T>(o / l);
+            o1[((size_t)bh * G + g0) * D + e] = o / l;
             if (c == 0) lse1[(size_t)bh * G + g0 + g] = m + logf(l);
         }
         if constexpr (ACCUM) {
@@ -261,8 +319,8 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
             } else if (pos >= 0) {
                 for (int s = lane; s < LPR; s += 32) {
                     float kf[E], vf[E];
-                    Row::load(blk + L.off_k, blk + L.off_kp, C, false, pos % W, s, kf);
-                    Row::load(blk + L.off_v, blk + L.off_vp, C, true, pos % W, s, vf);
+                    Row::unpack(Row::load(blk + L.off_k, blk + L.off_kp, false, pos % W, s), kf);
+                    Row::unpack(Row::load(blk + L.off_v, blk + L.off_vp, true, pos % W, s), vf);
 #pragma unroll
                     for (int e = 0; e < E; ++e) a += wt[Row::channel(false, s, e)] * kf[e] + wt[D + Row::channel(true, s, e)] * vf[e];
                 }
@@ -274,14 +332,13 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
 
     // ---- write-back ---------------------------------------------------------------------------------------------------
     __syncthreads();
-    constexpr int WORDS = FOUR ? D / 8 : D * (int)sizeof(T) / 4, GROUPS = FOUR ? D / kGroup4 : 0;   // 4-byte words of a row, of its parameters
+    constexpr int WORDS = FOUR ? D / 8 : D, GROUPS = FOUR ? D / kGroup4 : 0;   // 4-byte words of a row, of its parameters
     if (dst >= 0)
         for (int e = tid; e < 2 * (WORDS + GROUPS); e += DT) {
             const bool values = e >= WORDS + GROUPS, par = e % (WORDS + GROUPS) >= WORDS;
             const int w = e % (WORDS + GROUPS) - (par ? WORDS : 0), len = par ? GROUPS : WORDS;
             uint32_t* a = reinterpret_cast<uint32_t*>(blk + (par ? (values ? L.off_vp : L.off_kp) : (values ? L.off_v : L.off_k)));
-            auto at = [&](int row) { return (size_t)row * len + (!FOUR && sizeof(T) == 2 ? (cache_chunk_pos(C, row, w >> 2) << 2) | (w & 3) : w); };
-            a[at(W + dst)] = a[at(slot)];
+            a[(size_t)(W + dst) * len + w] = a[(size_t)slot * len + w];
         }
     __syncthreads();
     if constexpr (FOUR) {
@@ -294,8 +351,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
     } else {
         for (int e = tid; e < 2 * D; e += DT) {
             const bool values = e >= D;
-            const int c = e % D, at = sizeof(T) == 2 ? (cache_chunk_pos(C, slot, c >> 3) << 3) | (c & 7) : c;
-            reinterpret_cast<T*>(blk + (values ? L.off_v : L.off_k))[(size_t)slot * D + at] = (values ? v1 : k1)[(size_t)bh * D + c];
+            reinterpret_cast<float*>(blk + (values ? L.off_v : L.off_k))[(size_t)slot * D + e % D] = (values ? s_vn : s_kn)[e % D];
         }
     }
     if (tid == 0) {
@@ -322,18 +378,18 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
     const RowsRule rule = {decay, p.zthr, p.K, p.w, p.bias};
     if (p.dtype == LTE_BF16)
         return four ? launch_decode_rows4_bf16(p, accum, rule, cache, q1, k1, v1, o1, lse1, st) : launch_decode_rows_bf16(p, rule, cache, q1, k1, v1, o1, lse1, st);
-    const CacheLayout C = cache_layout(p.d, p.W, p.R, p.dtype);
-    const RowsLayout L = four ? rows_layout(cache4_layout(p.d, p.W, p.R)) : rows_layout(C);
+    const RowsLayout L = four ? rows_layout(cache4_layout(p.d, p.W, p.R)) : rows_layout(cache_layout(p.d, p.W, p.R, p.dtype));
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
-    const int BH = p.B * p.H, rows = p.W + p.R, nq = p.G < QP ? p.G : QP;
-    auto smem = [&](int split) { return (size_t)((rows + split - 1) / split) * (nq + (p.G > QP ? 1 : 0)) * 4; };
-    int nsplit = 1;
-    while (nsplit < MAX_SPLIT && (smem(nsplit) > 48 * 1024 || (BH * nsplit * 2 <= 2 * n_sm && rows / (nsplit * 2) >= 32))) nsplit *= 2;
-    auto go = [&](auto t, auto d, auto f4, auto acc) {
-        using T = decltype(t);
-        constexpr int D = decltype(d)::value;
-        auto kern = decode_rows_kernel<T, D, decltype(f4)::value, decltype(acc)::value>;
+    const int BH = p.B * p.H, rows = p.W + p.R;
+    auto go = [&](auto d, auto qp, auto f4, auto acc) {
+        constexpr int D = decltype(d)::value, QP = decltype(qp)::value;
+        const int nq = p.G < QP ? p.G : QP;
+        auto smem = [&](int split) { return (size_t)((rows + split - 1) / split) * (nq + (p.G > QP ? 1 : 0)) * 4; };
+        // two blocks an SM, each with 32 rows at least; more where a block's logits would take too much shared memory
+        int nsplit = 1;
+        while (nsplit < MAX_SPLIT && (smem(nsplit) > 48 * 1024 || (BH * nsplit * 2 <= 2 * n_sm && rows / (nsplit * 2) >= 32))) nsplit *= 2;
+        auto kern = decode_rows_kernel<D, QP, decltype(f4)::value, decltype(acc)::value>;
         static PerDeviceOnce once;
         if (int e = once.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024); })) return e;
         cudaLaunchConfig_t cfg = {};
@@ -344,22 +400,20 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = nsplit > 1 ? 2 : 1;
-        return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, C, (const T*)q1, (const T*)k1, (const T*)v1, (T*)o1, lse1, rule, p.H,
-                                              p.W, p.R, p.sink, p.scale, p.G, (rows + nsplit - 1) / nsplit));
+        return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const float*)q1, (const float*)k1, (const float*)v1, (float*)o1, lse1,
+                                              rule, p.H, p.W, p.R, p.sink, p.scale, p.G, (rows + nsplit - 1) / nsplit));
     };
-    auto kinds = [&](auto t, auto d) {
-        if (!four) return go(t, d, std::false_type(), std::true_type());   // (the learned rule over ordinary caches is lte_attn_decode)
-        return accum ? go(t, d, std::true_type(), std::true_type()) : go(t, d, std::true_type(), std::false_type());
+    auto kinds = [&](auto d, auto qp) {
+        if (!four) return go(d, qp, std::false_type(), std::true_type());   // (the learned rule over ordinary caches is lte_attn_decode)
+        return accum ? go(d, qp, std::true_type(), std::true_type()) : go(d, qp, std::true_type(), std::false_type());
     };
-    auto dims = [&](auto t) {
-        switch (p.d) {
-            case 32: return kinds(t, std::integral_constant<int, 32>());
-            case 64: return kinds(t, std::integral_constant<int, 64>());
-            case 128: return kinds(t, std::integral_constant<int, 128>());
-        }
-        return (int)LTE_ERR_UNSUPPORTED;
-    };
-    return dims(0.f);
+    auto heads = [&](auto d) { return p.G == 1 ? kinds(d, std::integral_constant<int, 1>()) : kinds(d, std::integral_constant<int, 4>()); };
+    switch (p.d) {
+        case 32: return heads(std::integral_constant<int, 32>());
+        case 64: return heads(std::integral_constant<int, 64>());
+        case 128: return heads(std::integral_constant<int, 128>());
+    }
+    return LTE_ERR_UNSUPPORTED;
 }
 
 }  // namespace lte
