@@ -262,7 +262,8 @@ int lte_attn_decode_accum(const lte_shape* s, float decay, void* cache, const vo
 
 /*
  * The decode cache in 4 bits: a head's rows take 1.25 d bytes in the place of 4 d (bf16).  A row is cut into groups of 32 channels:
- *   zero = bf16(min), step = bf16((max - min) / 15), code = clamp(rint((x - zero) / step), 0, 15) (fp32 arithmetic; 0 where step is 0),
+ *   zero = bf16(min), step = bf16((max - min) (1/15)), code = clamp(rint((x - zero) / step), 0, 15)
+ * (fp32 arithmetic, 1/15 the fp32 number next to it; 0 where step is 0),
  * and a channel reads back as zero + code step.  A group that holds a NaN or an infinity, or whose step or zero is not finite in bf16,
  * reads back as NaN.  Scores (logits, or accumulated attention), positions and counters are those of the ordinary cache.
  *

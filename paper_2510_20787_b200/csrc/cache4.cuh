@@ -1,6 +1,7 @@
 // The decode cache in 4 bits: where things stand in it, and the rule by which a row is rounded (see lte_cache4_bytes in lte.h).
 //
-// A row is cut into groups of 32 channels, each with two bf16 parameters, zero = bf16(min) and step = bf16((max - min) / 15); a channel is a
+// A row is cut into groups of 32 channels, each with two bf16 parameters, zero = bf16(min) and step = bf16((max - min) (1/15)), 1/15 and
+// the product rounded to fp32; a channel is a
 // 4-bit code c and stands for zero + c step.  Why this form: 32 channels keep the largest of them from setting the step of the
 // whole row, at 4 bytes of parameters to 16 of codes; both parameters in bf16 have the range of the rows themselves (fp16 would overflow or
 // lose small rows), and c step has at most 12 bits, so that the value is exact up to one rounding of the sum.  zero differs from the minimum
@@ -56,7 +57,7 @@ __device__ __forceinline__ float value4(uint32_t code, uint32_t par) { return fm
 // back as NaN.
 __device__ __forceinline__ uint32_t group4(float lo, float hi, bool bad)
 {
-    const uint32_t step = __bfloat16_as_ushort(__float2bfloat16_rn(__fdiv_rn(hi - lo, 15.f)));
+    const uint32_t step = __bfloat16_as_ushort(__float2bfloat16_rn((hi - lo) * (1.f / 15.f)));
     const uint32_t zero = __bfloat16_as_ushort(__float2bfloat16_rn(lo));
     if (bad || (step & 0x7f80u) == 0x7f80u || (zero & 0x7f80u) == 0x7f80u) return 0x7fc07fc0u;
     return step | (zero << 16);

@@ -75,7 +75,7 @@ def four(x):
     g = x.reshape(-1, 32)
     bf = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(torch.bfloat16).float().numpy()  # noqa: E731
     with np.errstate(all="ignore"):
-        step, zero = bf((g.max(1) - g.min(1)) / np.float32(15)), bf(g.min(1))
+        step, zero = bf((g.max(1) - g.min(1)) * (np.float32(1) / np.float32(15))), bf(g.min(1))
         bad = ~(np.isfinite(step) & np.isfinite(zero) & np.isfinite(g).all(1))
         code = np.clip(np.rint((g - zero[:, None]) / np.where(step > 0, step, 1)[:, None]), 0, 15)
     code = np.where((step > 0)[:, None] & ~bad[:, None], code, 0)
