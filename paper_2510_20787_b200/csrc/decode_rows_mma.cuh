@@ -37,7 +37,7 @@ namespace {
 
 constexpr int MQ = 8;                                          // query heads per pass
 // resident warps the registers (and the stages in shared memory) are budgeted for
-__host__ __device__ constexpr int warps_per_sm(int d, bool four) { return d == 128 ? 8 : 16; }
+__host__ __device__ constexpr int warps_per_sm(int d, bool four) { return d == 128 && four ? 8 : 16; }
 constexpr int MAX_WARPS = 8;                                   // per block
 // blocks of so many warps come in clusters (at d = 128 eight warps take an SM's registers, and the next step's blocks then find no room beside them)
 __host__ __device__ constexpr bool clusters(int d, int nw) { return nw == MAX_WARPS || (d == 128 && nw == 4); }
@@ -51,11 +51,11 @@ struct Rows {
     int total;
 };
 template <int D, bool FOUR> struct Stage {
-    static constexpr int UR = FOUR ? 32 : 16, STAGES = FOUR ? 3 : 2;
+    static constexpr int UR = FOUR ? 32 : 16, STAGES = D < 128 ? 2 : FOUR ? 3 : 1;
     static constexpr int ROW = FOUR ? D / 2 : 2 * D, PAR = FOUR ? D / 8 : 0;   // bytes of a row's keys, of its key parameters
     static constexpr int K = 0, V = UR * ROW, KP = 2 * V, VP = KP + UR * PAR, BYTES = VP + UR * PAR;
     static constexpr int ACC = MQ * (D + 8) * 4;               // a warp's outputs stand where its stages were
-    static_assert(ACC <= STAGES * BYTES, "");
+    static_assert(ACC <= STAGES * BYTES, "the outputs' place");
 };
 
 // The two products with a span of 16 rows that stands in shared memory, lane (g, t) = (lane / 4, lane % 4).  Rows past the last one and those that the
@@ -88,7 +88,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 #pragma unroll
             for (int j = 0; j < KP; ++j)
                 k[u][j] = *reinterpret_cast<const uint4*>(st + Stage<D, false>::K + (16 * span + g + 8 * u) * PITCH + (((t + 4 * j) ^ (SWZ ? g & 7 : 0)) << 4));
-        constexpr int NS = D == 128 ? 2 * KP : 1;
+        constexpr int NS = D == 128 ? 2 : 1;
         float cs[NS][4];
 #pragma unroll
         for (int i = 0; i < 2 * KP; ++i) {
@@ -370,39 +370,35 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     const int step = NW * nsplit, first = wid * nsplit + rank;
     unsigned char* const stage = s_dyn + wid * (St::STAGES * St::BYTES);
     const uint32_t stage_at = tc::smem_u32(stage);
-    auto ask = [&](int i, int s) {                             // unit i of the head into stage s
+    // keys (values) and their parameters of unit i of the head into stage s
+    auto ask = [&](int i, int s, auto values) {
+        constexpr bool V = decltype(values)::value;
         const int n_rows = rows.total - UR * i;
-        const uint32_t to = stage_at + s * St::BYTES + 16 * lane;
-        const unsigned char *fk = rows.K + (size_t)i * (UR * St::ROW) + 16 * lane, *fv = rows.V + (size_t)i * (UR * St::ROW) + 16 * lane;
-        auto rows_of = [&](auto whole) {
-            constexpr int N = UR * St::ROW / 512;              // pieces of keys (of values) a lane copies
+        const uint32_t to = stage_at + s * St::BYTES + (V ? St::V : St::K) + 16 * lane;
+        const unsigned char* from = (V ? rows.V : rows.K) + (size_t)i * (UR * St::ROW) + 16 * lane;
+        auto copy = [&](auto whole) {
+            constexpr bool ALL = decltype(whole)::value;
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const bool there = decltype(whole)::value || 16 * lane + 512 * u < n_rows * St::ROW;
-                if (there) tc::cp_async16(to + St::K + 512 * u, fk + 512 * u, 16);
-                if (there) tc::cp_async16(to + St::V + 512 * u, fv + 512 * u, 16);
-            }
-            if constexpr (FOUR) {                              // both parameters at once: they lie behind each other in the stage
-                constexpr int P = UR * St::PAR;                // bytes of one (the last 16 of a part of the cache are its own)
-#pragma unroll
-                for (int u = 0; u < (2 * P + 511) / 512; ++u) {
-                    const int b = 16 * lane + 512 * u, at = b < P ? b : b - P;
-                    if (b < 2 * P && (decltype(whole)::value || at < n_rows * St::PAR))
-                        tc::cp_async16(to + St::KP + 512 * u, (b < P ? rows.KP : rows.VP) + (size_t)i * P + at, 16);
-                }
+            for (int u = 0; u < UR * St::ROW / 512; ++u)
+                if (ALL || 16 * lane + 512 * u < n_rows * St::ROW) tc::cp_async16(to + 512 * u, from + 512 * u, 16);
+            if constexpr (FOUR) {
+                constexpr int P = UR * St::PAR;                // (the last 16 bytes of a part of the cache are its own)
+                if ((P >= 512 || 16 * lane < P) && (ALL || 16 * lane < n_rows * St::PAR))
+                    tc::cp_async16(to + ((V ? St::VP : St::KP) - (V ? St::V : St::K)), (V ? rows.VP : rows.KP) + (size_t)i * P + 16 * lane, 16);
             }
         };
-        if (n_rows >= UR) rows_of(std::true_type());
-        else rows_of(std::false_type());
+        if (n_rows >= UR) copy(std::true_type());
+        else if (n_rows > 0) copy(std::false_type());
+        tc::cp_async_commit();                                 // (one group per call, whether there is anything to copy or not)
     };
-    auto begin = [&](int units_there) {                        // the first units of a pass
+    auto begin = [&]() {                                       // the first units of a pass
 #pragma unroll
         for (int b = 0; b < St::STAGES; ++b) {
-            if (first + b * step < units_there) ask(first + b * step, b);
-            tc::cp_async_commit();
+            ask(first + b * step, b, std::false_type());
+            ask(first + b * step, b, std::true_type());
         }
     };
-    begin((rows.total + UR - 1) / UR);
+    begin();
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
     typename Gr::Query qf;
     Gr::load_q(qf, q1 + (size_t)bh * G * D, g < G, g, t);
@@ -565,7 +561,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         if (g0 > 0) {                                          // further query heads read the rows again
             Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
             __syncthreads();                                   // the previous pass's outputs, which stand in the stages, have been combined
-            begin(units);
+            begin();
         }
         if (rank == 0)                                         // the incoming token's logits
             for (int u = wid; u < nq; u += NW) {
@@ -589,10 +585,12 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
             const unsigned char* st = stage + at_stage * St::BYTES;
-            tc::cp_async_wait<St::STAGES - 1>();
-            __syncwarp();                                      // every lane's copies of this unit are there
+            tc::cp_async_wait<2 * St::STAGES - 1>();
+            __syncwarp();                                      // every lane's copies of this unit's keys are there
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
+            __syncwarp();                                      // every lane has read the keys
+            ask(i + St::STAGES * step, at_stage, std::false_type());
             unsigned gone = 0;                                 // rows of the unit that do not count
             if (i >= full || i == masked_ring / UR || i == masked_pool / UR) {
                 if (i >= full) gone = ~0u << (rows.total - UR * i);
@@ -613,6 +611,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 }
                 kept += UR;
             }
+            tc::cp_async_wait<2 * St::STAGES - 1>();
+            __syncwarp();                                      // ... of its values
             typename Gr::Pars vpar[UNIT];
             float steps = 0.f;
 #pragma unroll
@@ -644,9 +644,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             }
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
-            __syncwarp();                                      // every lane has read the stage
-            if (i + St::STAGES * step < units) ask(i + St::STAGES * step, at_stage);
-            tc::cp_async_commit();
+            __syncwarp();
+            ask(i + St::STAGES * step, at_stage, std::true_type());
             at_stage = at_stage + 1 == St::STAGES ? 0 : at_stage + 1;
         }
         tc::cp_async_wait<0>();                                // (units asked for before it was known how many rows are in use)
@@ -813,12 +812,12 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, MEASURED.  16 heads x 1,024 rows take
     // 7.9 us with four warps in clusters of 8, 13.1 with eight.
     const bool is_long = rows > 4096;
-    const int most_w = p.d == 128 && !is_long ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
+    const int most_w = p.d == 128 && (FOUR || !is_long) ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
     int nw = 1, nsplit = 1;
     for (int c : {2, 4, 8})
         if (c <= most_w && ((BH <= n_sm * (wps / c) && rows / c >= 16) || smem(c / 2, 1) * (wps / (c / 2)) > 96 * 1024)) nw = c;
     if (nw == most_w)
-        while (nsplit < most_split && ((BH * nw * nsplit * 2 <= warps && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
+        while (nsplit < most_split && ((BH * nw * nsplit * 2 <= (nsplit < 8 ? warps : warps / 2) && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
         {
