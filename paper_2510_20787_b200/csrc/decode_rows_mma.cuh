@@ -51,11 +51,11 @@ struct Rows {
     int total;
 };
 template <int D, bool FOUR> struct Stage {
-    static constexpr int UR = FOUR ? 32 : 16, STAGES = D < 128 ? 2 : FOUR ? 3 : 1;
+    static constexpr int UR = FOUR ? 32 : 16;
     static constexpr int ROW = FOUR ? D / 2 : 2 * D, PAR = FOUR ? D / 8 : 0;   // bytes of a row's keys, of its key parameters
     static constexpr int K = 0, V = UR * ROW, KP = 2 * V, VP = KP + UR * PAR, BYTES = VP + UR * PAR;
     static constexpr int ACC = MQ * (D + 8) * 4;               // a warp's outputs stand where its stages were
-    static_assert(ACC <= STAGES * BYTES, "the outputs' place");
+    static_assert(ACC <= BYTES, "the outputs' place");
 };
 
 // The two products with a span of 16 rows that stands in shared memory, lane (g, t) = (lane / 4, lane % 4).  Rows past the last one and those that the
@@ -327,7 +327,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
 };
 
-template <int D, int NW, bool SWZ, bool FOUR, bool ACCUM>
+template <int D, int NW, int STAGES, bool SWZ, bool FOUR, bool ACCUM>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
@@ -339,8 +339,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     constexpr int UR = St::UR, UNIT = UR / 16;
     constexpr int SPLIT = clusters(D, NW) ? MAX_SPLIT : 1;
     extern __shared__ __align__(128) unsigned char s_dyn[];    // the warps' stages; [NW][nq][most + 4] logits, behind them [NW][most + 4] sums over passes
-    float* const s_log = reinterpret_cast<float*>(s_dyn + NW * St::STAGES * St::BYTES);
-    auto s_acc = [&](int w, int u) { return reinterpret_cast<float*>(s_dyn + w * (St::STAGES * St::BYTES)) + u * PITCH; };
+    float* const s_log = reinterpret_cast<float*>(s_dyn + NW * STAGES * St::BYTES);
+    auto s_acc = [&](int w, int u) { return reinterpret_cast<float*>(s_dyn + w * (STAGES * St::BYTES)) + u * PITCH; };
     __shared__ float s_unit[MQ];
     __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
     __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
     rows.total = W + R;
     const int step = NW * nsplit, first = wid * nsplit + rank;
-    unsigned char* const stage = s_dyn + wid * (St::STAGES * St::BYTES);
+    unsigned char* const stage = s_dyn + wid * (STAGES * St::BYTES);
     const uint32_t stage_at = tc::smem_u32(stage);
     // keys (values) and their parameters of unit i of the head into stage s
     auto ask = [&](int i, int s, auto values) {
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     };
     auto begin = [&]() {                                       // the first units of a pass
 #pragma unroll
-        for (int b = 0; b < St::STAGES; ++b) {
+        for (int b = 0; b < STAGES; ++b) {
             ask(first + b * step, b, std::false_type());
             ask(first + b * step, b, std::true_type());
         }
@@ -585,12 +585,12 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
             const unsigned char* st = stage + at_stage * St::BYTES;
-            tc::cp_async_wait<2 * St::STAGES - 1>();
+            tc::cp_async_wait<2 * STAGES - 1>();
             __syncwarp();                                      // every lane's copies of this unit's keys are there
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
             __syncwarp();                                      // every lane has read the keys
-            ask(i + St::STAGES * step, at_stage, std::false_type());
+            ask(i + STAGES * step, at_stage, std::false_type());
             unsigned gone = 0;                                 // rows of the unit that do not count
             if (i >= full || i == masked_ring / UR || i == masked_pool / UR) {
                 if (i >= full) gone = ~0u << (rows.total - UR * i);
@@ -611,7 +611,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 }
                 kept += UR;
             }
-            tc::cp_async_wait<2 * St::STAGES - 1>();
+            tc::cp_async_wait<2 * STAGES - 1>();
             __syncwarp();                                      // ... of its values
             typename Gr::Pars vpar[UNIT];
             float steps = 0.f;
@@ -645,8 +645,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
             __syncwarp();
-            ask(i + St::STAGES * step, at_stage, std::true_type());
-            at_stage = at_stage + 1 == St::STAGES ? 0 : at_stage + 1;
+            ask(i + STAGES * step, at_stage, std::true_type());
+            at_stage = at_stage + 1 == STAGES ? 0 : at_stage + 1;
         }
         tc::cp_async_wait<0>();                                // (units asked for before it was known how many rows are in use)
         __syncwarp();
@@ -820,8 +820,9 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         while (nsplit < most_split && ((BH * nw * nsplit * 2 <= (nsplit < 8 ? warps : warps / 2) && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
-        {
-            auto kern = decode_rows_mma_kernel<D, NW, decltype(s)::value, FOUR, ACCUM>;
+        auto with = [&](auto stages) {
+            constexpr int STAGES = decltype(stages)::value;
+            auto kern = decode_rows_mma_kernel<D, NW, STAGES, decltype(s)::value, FOUR, ACCUM>;
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -846,14 +847,20 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
                     return (int)LTE_OK; })) return e;
             const int split = nsplit < split_most ? nsplit : split_most;
             cfg.gridDim = dim3(BH * split); cfg.blockDim = dim3(NW * 32); cfg.stream = st;
-            cfg.dynamicSmemBytes = smem(nw, split) + NW * Stage<D, FOUR>::STAGES * Stage<D, FOUR>::BYTES;
+            cfg.dynamicSmemBytes = smem(nw, split) + NW * STAGES * Stage<D, FOUR>::BYTES;
             if (cfg.dynamicSmemBytes > kMostSmem) return (int)LTE_ERR_UNSUPPORTED;
             attr[1].val.clusterDim.x = split;
             cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
             return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
                                                   (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
                                                   most(nw * split)));
-        }
+        };
+        // two stages a warp; three where eight warps of an SM have the room, one where 16 have not (bf16 at d = 128: 8 KB a stage), unless few
+        // heads leave it: 16 x 1,024 rows MEASURED
+        if constexpr (D < 128) return with(std::integral_constant<int, 2>());
+        else if constexpr (FOUR) return with(std::integral_constant<int, 3>());
+        else if constexpr (NW == 4) return BH * nsplit * NW <= 8 * n_sm ? with(std::integral_constant<int, 2>()) : with(std::integral_constant<int, 1>());
+        else return with(std::integral_constant<int, 1>());
     };
     auto widths = [&](auto d, auto s) {
         switch (nw) {
