@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(PT) cache4_pack_kernel(const unsigned char* __
             uint32_t par;
             if constexpr (sizeof(T) == 2) par = group4_of(p[u][values].u[0]);
             else par = group4_of(f);
-            const uint32_t w = codes4(f, par);
+            const uint32_t w = codes4<sizeof(T) == 2>(f, par);
             if (row < rows) {
                 unsigned char* codes = dst + (values ? Q.off_v : Q.off_k) + (size_t)row * (D / 2);
                 if (values) {

@@ -76,7 +76,8 @@ __device__ __forceinline__ uint32_t code4(float x, uint32_t par)
 // between k + 1/2 and its neighbour, a number of 25 bits, which times step is no fp32 number d (step has 8 bits, so that what is not on
 // the border is further off).  Rounding is by adding 1.5 2^23, which leaves the code in the lowest bits.  Steps outside 2^-100 .. 2^100, where
 // the terms might leave the range of fp32, are divided by.
-__device__ __forceinline__ uint32_t codes4(const float (&f)[8], uint32_t par)
+// EXACT: the channels are bf16 numbers.  zero is then the minimum itself, and quotients lie between 0 and 15 (1 + 2^-8): nothing to clamp.
+template <bool EXACT> __device__ __forceinline__ uint32_t codes4(const float (&f)[8], uint32_t par)
 {
     constexpr float MAGIC = 12582912.f;
     constexpr uint32_t REST = 0x4b400000u * 0x11111111u;       // (modulo 2^32: what the bits above the codes add up to)
@@ -87,7 +88,7 @@ __device__ __forceinline__ uint32_t codes4(const float (&f)[8], uint32_t par)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float d = f[i] - zero, q0 = d * y, q = fmaf(fmaf(-q0, step, d), y, q0);
-            w += __float_as_uint(fminf(fmaxf(q, 0.f), 15.f) + MAGIC) << (4 * i);
+            w += __float_as_uint((EXACT ? q : fminf(fmaxf(q, 0.f), 15.f)) + MAGIC) << (4 * i);
         }
     } else if (step > 0.f) {
 #pragma unroll 1

@@ -233,8 +233,8 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
                 const float s = par4_step(kp[i][j]), z = par4_zero(kp[i][j]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float v = fmaf(s, p[2 * i + e], z * Q.sum[j][e]);
-                    c[2 * i + e] = j == 0 ? v : c[2 * i + e] + v;
+                    const float v = j == 0 ? z * Q.sum[j][e] : fmaf(z, Q.sum[j][e], c[2 * i + e]);
+                    c[2 * i + e] = fmaf(s, p[2 * i + e], v);
                 }
             }
         }
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 #pragma unroll
             for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(word(u, i) << 16); f[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
             new_par = group4_of(u);
-            new_codes = codes4(f, new_par);
+            new_codes = codes4<true>(f, new_par);
         }
     }
 

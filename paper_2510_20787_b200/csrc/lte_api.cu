@@ -488,10 +488,18 @@ size_t lte_cache4_bytes(const lte_shape* s)
     return L.header + (size_t)s->B * s->H * L.stride;
 }
 
+// two caches, each whole and apart from the other
+static bool two_caches(const lte_shape* s, const void* cache, const void* cache4)
+{
+    if (!cache || !cache4 || !aligned16(cache) || !aligned16(cache4)) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(cache), b = reinterpret_cast<uintptr_t>(cache4);
+    return a < b ? b - a >= lte_cache_bytes(s) : a - b >= lte_cache4_bytes(s);
+}
+
 int lte_cache4_pack(const lte_shape* s, const void* cache, void* cache4, void* stream)
 {
     int e = check_rows(s); if (e) return e;
-    if (!cache || !cache4 || cache == cache4 || !aligned16(cache) || !aligned16(cache4)) return LTE_ERR_INVALID_ARG;
+    if (!two_caches(s, cache, cache4)) return LTE_ERR_INVALID_ARG;
     e = check_arch(); if (e) return e;
     return launch_cache4_pack(make_params(s, nullptr), cache, cache4, (cudaStream_t)stream);
 }
@@ -499,7 +507,7 @@ int lte_cache4_pack(const lte_shape* s, const void* cache, void* cache4, void* s
 int lte_cache4_unpack(const lte_shape* s, const void* cache4, void* cache, void* stream)
 {
     int e = check_rows(s); if (e) return e;
-    if (!cache || !cache4 || cache == cache4 || !aligned16(cache) || !aligned16(cache4)) return LTE_ERR_INVALID_ARG;
+    if (!two_caches(s, cache, cache4)) return LTE_ERR_INVALID_ARG;
     e = check_arch(); if (e) return e;
     return launch_cache4_unpack(make_params(s, nullptr), cache4, cache, (cudaStream_t)stream);
 }

@@ -62,6 +62,8 @@ def test_refusals():
         assert f(None, FAKE, 2 * FAKE, None) == f(a(s), None, FAKE, None) == f(a(s), FAKE, None, None) == -1
         assert f(a(s), FAKE, FAKE, None) == f(a(s), FAKE + 8, 2 * FAKE, None) == f(a(s), FAKE, 2 * FAKE + 8, None) == -1
         assert f(a(odd), FAKE, 2 * FAKE, None) == -2
+        first = lte.lte_cache_bytes(s) if f is L.lte_cache4_pack else lte.lte_cache4_bytes(s)
+        assert f(a(s), FAKE, FAKE + first - 16, None) == -1    # overlapping
 
 
 @pytest.mark.parametrize("d,W,R", [(32, 16, 8), (64, 768, 512), (128, 77, 41), (32, 5, 0), (32, 1, 2)])
