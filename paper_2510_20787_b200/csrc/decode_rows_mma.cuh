@@ -51,7 +51,7 @@ struct Rows {
     int total;
 };
 template <int D, bool FOUR> struct Stage {
-    static constexpr int UR = FOUR ? 32 : 16;
+    static constexpr int UR = FOUR || D < 128 ? 32 : 16;
     static constexpr int ROW = FOUR ? D / 2 : 2 * D, PAR = FOUR ? D / 8 : 0;   // bytes of a row's keys, of its key parameters
     static constexpr int K = 0, V = UR * ROW, KP = 2 * V, VP = KP + UR * PAR, BYTES = VP + UR * PAR;
     static constexpr int ACC = MQ * (D + 8) * 4;               // a warp's outputs stand where its stages were
@@ -805,7 +805,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     int n_sm = 0;
     if (int e = device_sm_count(&n_sm)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm;
-    constexpr int UR = Stage<64, FOUR>::UR;                    // rows that a warp takes at a time
+    const int UR = FOUR || p.d < 128 ? 32 : 16;                // rows that a warp takes at a time (Stage::UR)
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
     auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
     auto smem = [&](int nw, int split) { return (size_t)nw * (most(nw * split) + 4) * kept * 4; };   // of logits
@@ -857,7 +857,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         };
         // two stages a warp; three where eight warps of an SM have the room, one where 16 have not (bf16 at d = 128: 8 KB a stage), unless few
         // heads leave it: 16 x 1,024 rows MEASURED
-        if constexpr (D < 128) return with(std::integral_constant<int, 2>());
+        if constexpr (D < 128) return with(std::integral_constant<int, FOUR || D == 32 ? 2 : 1>());
         else if constexpr (FOUR) return with(std::integral_constant<int, 3>());
         else if constexpr (NW == 4) return BH * nsplit * NW <= 8 * n_sm ? with(std::integral_constant<int, 2>()) : with(std::integral_constant<int, 1>());
         else return with(std::integral_constant<int, 1>());
