@@ -39,7 +39,8 @@ constexpr int MQ = 8;                                          // query heads pe
 // resident warps the registers (and the stages in shared memory) are budgeted for
 __host__ __device__ constexpr int warps_per_sm(int d, bool four) { return d == 128 && four ? 8 : 16; }
 constexpr int MAX_WARPS = 8;                                   // per block
-// blocks of so many warps come in clusters (at d = 128 eight warps take an SM's registers, and the next step's blocks then find no room beside them)
+// blocks of so many warps come in clusters (at d = 128 with four already: eight 4-bit ones take an SM's registers, and the next step's blocks then
+// find no room beside them)
 __host__ __device__ constexpr bool clusters(int d, int nw) { return nw == MAX_WARPS || (d == 128 && nw == 4); }
 constexpr int MAX_SPLIT = 16;                                  // blocks per head
 
@@ -331,7 +332,7 @@ template <int D, int NW, int STAGES, bool SWZ, bool FOUR, bool ACCUM>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
-    float scale, int G, int most)                              // most: rows whose logits a warp keeps (whole spans)
+    float scale, int G, int most)                              // most: rows whose logits a warp may have to keep (whole units)
 {
     using Gr = Group<D, SWZ, FOUR>;
     constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
@@ -698,16 +699,16 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         if (!shared_head && wid == 0 && lane < nq) lse1[(size_t)bh * G + g0 + lane] = qm * (scale * s_unit[lane]) + logf(qt);
         for (int e = tid; e < nq * D; e += NT) {               // (a warp's elements are of one query)
             const int u = e / D, ch = e - u * D;
-            const float m = __shfl_sync(0xffffffffu, qm, u), tot = __shfl_sync(0xffffffffu, shared_head ? qt : qi, u), sq = __shfl_sync(0xffffffffu, qs, u);
+            const float m = __shfl_sync(0xffffffffu, qm, u), sum = __shfl_sync(0xffffffffu, qt, u), sq = __shfl_sync(0xffffffffu, qs, u);
             float o = rank == 0 ? exp2_fast((s_new[u] - m) * sq) * __bfloat162float(s_kv[1][ch]) : 0.f;
 #pragma unroll
             for (int w2 = 0; w2 < NW; ++w2) o = fmaf(exp2_fast((s_m[w2][u] - m) * sq), s_acc(w2, u)[ch], o);
             if (!shared_head) {
-                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * tot);
+                o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * __shfl_sync(0xffffffffu, qi, u));
             } else {                                           // into the shared memory of the block that finishes this element
                 const int own = e / per;
                 *cluster.map_shared_rank(&s_in[par][rank * per + (e - own * per)], own) = o;
-                if (ch < nsplit) *reinterpret_cast<float2*>(cluster.map_shared_rank(&s_ml[par][rank][u][0], ch)) = make_float2(m, tot);
+                if (ch < nsplit) *reinterpret_cast<float2*>(cluster.map_shared_rank(&s_ml[par][rank][u][0], ch)) = make_float2(m, sum);
             }
         }
         if (shared_head) {
