@@ -1,11 +1,10 @@
 // The decode cache in 4 bits: where things stand in it, and the rule by which a row is rounded (see lte_cache4_bytes in lte.h).
 //
-// A row is cut into groups of 32 channels, each with two bf16 parameters, zero = bf16(min) and step = bf16((max - min) (1/15)), 1/15 and
-// the product rounded to fp32; a channel is a
-// 4-bit code c and stands for zero + c step.  Why this form: 32 channels keep the largest of them from setting the step of the
-// whole row, at 4 bytes of parameters to 16 of codes; both parameters in bf16 have the range of the rows themselves (fp16 would overflow or
-// lose small rows), and c step has at most 12 bits, so that the value is exact up to one rounding of the sum.  zero differs from the minimum
-// by half a bf16 step at most (2^-9 of it), which for a group around 0 is a hundredth of `step`.
+// A row is cut into groups of 32 channels, each with two bf16 parameters, zero = bf16(min) and step = bf16((max - min) (1/15)), 1/15 and the product
+// rounded to fp32; a channel is a 4-bit code c and stands for zero + c step.  Why this form: 32 channels keep the largest of them from setting the
+// step of the whole row, at 4 bytes of parameters to 16 of codes; both parameters in bf16 have the range of the rows themselves (fp16 would overflow
+// or lose small rows), and c step has at most 12 bits, so that the value is exact up to one rounding of the sum.  zero is the minimum itself for
+// bf16 rows, and within 2^-9 of it for fp32 ones, which for a group around 0 is a hundredth of `step`.
 //
 // The order of the codes is that of the tensor-core decode kernel's operands, which take them from memory without a shuffle:
 //   keys    4-byte word j of a row: group j mod (d/32), channels 8t .. 8t+7 of it with t = j / (d/32), lowest nibble first

@@ -6,7 +6,8 @@
 // A row is shared by the LPR lanes that hold its 16-byte pieces (4 bits: its 4-byte words).  What bounds it is the latency of its loads and the sums over
 // those lanes: a thread has BATCH rows in flight, and their partial sums for all query heads are added up together, half of them handed to
 // the other half of the lanes in every round (15 shuffles in the place of 64 for four rows, four query heads and 16 lanes).
-// Measured (B200, a step in a CUDA graph): MEASURED_F32
+// Measured (B200, a step in a CUDA graph; before: a row at a time): 64 heads x 1,280 rows, four query heads each, d = 64 23.0 us (43 MB: 6.6 at 6.56 TB/s),
+// before 39.5; 256 x 256 13.8 us (5.3), before 27.8; 2 heads x 24 rows, d = 32 5.8 us, before 6.3.
 #include <cfloat>
 #include <cooperative_groups.h>
 

@@ -2,7 +2,8 @@
 // operands, as in decode_mma.cu, every query head of a group at once, heads split over warps and clusters where there are few.
 //
 // Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there the instructions that unpack and weigh them count for more
-// (see the figures at the launch).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
+// (about 230 per 16 rows at d = 64, of which the two products' operands are 80, and 2,000 a warp beside them, at 0.55 per cycle: 14 warps an SM do not
+// hide their latencies, and registers for more are not there).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
 // through stages of its own in shared memory, keeps its own reference, sum and output, and meets the others once at the end.  The incoming token
 // is no row: its logit is a dot product on the fp32 ALUs, and it joins where the warps meet.
 //
@@ -20,6 +21,18 @@
 //            against 64 bits: 1.7e-3 before and after).  It is scaled by a power of two, the same for the warp, that follows the largest step.
 // The contraction index may be permuted freely: the nibbles i and i + 4 of a key word are neighbours in it, and so are the two rows whose value
 // units a byte permute joins.  The order of the codes in the cache (cache4.cuh) makes these the words that a lane loads.
+//
+// Measured (B200, us a step in a CUDA graph of steps over three caches in turn, full pools; bytes that cannot be avoided at 6.56 TB/s):
+//                                                    accumulated, bf16    4 bits, accumulated    4 bits, learned
+//   2,048 heads x 256 rows, d = 64                       28.5 (21.5)          21.7 (7.2)            20.9 (6.7)
+//   256 x 1,280, four query heads each, d = 64           22.0 (13.3)          15.5 (4.5)            14.2 (4.2)
+//   2,048 x 1,024, d = 64                                 107 (85.3)          66.5 (28.8)           58.3 (26.9)
+//   512 x 1,024, d = 128                                 48.5 (41.9)          30.7 (13.6)
+//   8 x 17,408, four query heads each, d = 128           30.9 (11.1)          24.1 (3.7)            19.9 (3.6)
+//   16 x 1,024, d = 128 (one user)                        9.3 (1.3)            8.8 (0.4)             8.2 (0.4)
+// Of a step about 5 us are the chain of launch, counters, first rows, meeting and write-back (32 rows a head: 5.1 to 8).  What did not help: 4-bit
+// rows in 80 registers and 24 warps an SM (2,048 x 256: 27.8), bulk copies with a barrier per stage in the place of 16-byte ones (the same for bf16,
+// and 35 instructions per 16 rows more), codes as bf16 numbers 16 + c with P in two terms (1.05 us per 16 rows of 2,048 heads, now 0.72).
 #pragma once
 #include <cfloat>
 #include <cooperative_groups.h>
@@ -810,8 +823,9 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
     auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
     auto smem = [&](int nw, int split) { return (size_t)nw * (most(nw * split) + 4) * kept * 4; };   // of logits
-    // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, MEASURED.  16 heads x 1,024 rows take
-    // 7.9 us with four warps in clusters of 8, 13.1 with eight.
+    // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, take 39.5 us with four warps,
+    // 30.9 with eight (bf16; 4-bit blocks of eight take an SM's registers: 24.1 and 33.0).  16 heads x 1,024 rows take 7.9 us with four warps in
+    // clusters of 8 and 13.1 with eight (4 bits, d = 128).  Clusters of 16 only where each block has an SM to itself: 16 heads took as long as 32.
     const bool is_long = rows > 4096;
     const int most_w = p.d == 128 && (FOUR || !is_long) ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
     int nw = 1, nsplit = 1;
@@ -857,7 +871,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
                                                   most(nw * split)));
         };
         // two stages a warp; three where eight warps of an SM have the room, one where 16 have not (bf16 at d = 128: 8 KB a stage), unless few
-        // heads leave it: 16 x 1,024 rows MEASURED
+        // heads leave it (16 x 1,024 rows: 9.7 us with one, 9.3 with two)
         if constexpr (D < 128) return with(std::integral_constant<int, FOUR || D == 32 ? 2 : 1>());
         else if constexpr (FOUR) return with(std::integral_constant<int, 3>());
         else if constexpr (NW == 4) return BH * nsplit * NW <= 8 * n_sm ? with(std::integral_constant<int, 2>()) : with(std::integral_constant<int, 1>());
