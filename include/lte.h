@@ -251,7 +251,7 @@ int lte_attn_decode(const lte_shape* s, const lte_conv* c, void* cache,
  *   a        in   [B,H,T] fp32 (idx, cnt as written by lte_select_rule)
  *   decay    0 .. 1
  *   cache    in/out;   q1, k1, v1, o1, lse1 as for lte_attn_decode
- * Deterministic.  A cache in this state does not go through the calls that read logits (lte_attn_decode, lte_attn_prefill_chunk,
+ * Deterministic.  A score that is NaN (of a head whose logits were) ranks above every number.  A cache in this state does not go through the calls that read logits (lte_attn_decode, lte_attn_prefill_chunk,
  * lte_cache_score): they would take a for logits.
  * Errors: INVALID_ARG (decay outside 0 .. 1), UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
  */
