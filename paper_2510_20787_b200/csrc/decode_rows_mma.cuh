@@ -82,7 +82,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     struct Query { uint4 f[KP]; float unit[2]; };              // pieces t, t + 4, .. of query g
     struct Acc { float a[MT][4]; };
     struct Pars {};
-    static __device__ __forceinline__ float load_pars(Pars&, const unsigned char*, int, unsigned, int) { return 0.f; }
+    static __device__ __forceinline__ float load_pars(Pars&, const unsigned char*, int, int) { return 0.f; }
     static __device__ __forceinline__ bool too_large(const Acc&, float) { return false; }
     static __device__ __forceinline__ void lower(Acc&, float) {}
     static __device__ __forceinline__ int rho(int g) { return g; }
@@ -131,8 +131,14 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 #pragma unroll
         for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
     }
-    // gone: bit r: row r of the span does not count.  Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, const unsigned char* st, int span, unsigned gone, int g, int t)
+    // what the rows of a unit that `gone` names hold as values
+    static __device__ __forceinline__ void clear(unsigned char* st, unsigned gone, int lane)
+    {
+        for (; gone; gone &= gone - 1u)
+            if (lane < D / 8) *reinterpret_cast<uint4*>(st + Stage<D, false>::V + (__ffs(gone) - 1) * PITCH + 16 * lane) = make_uint4(0, 0, 0, 0);
+    }
+    // Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, const unsigned char* st, int span, int g, int t)
     {
         uint32_t v[4][VB];
 #pragma unroll
@@ -151,12 +157,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
                 }
             }
         }
-        if (gone)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if ((gone >> (2 * t + (u & 1) + 8 * (u >> 1))) & 1u)
-#pragma unroll
-                    for (int j = 0; j < VB; ++j) v[u][j] = 0u;
         const uint32_t hi0 = pack_bf16(p[0], p[1]), hi1 = pack_bf16(p[2], p[3]);
         const uint32_t lo0 = pack_bf16(p[0] - __uint_as_float(hi0 << 16), p[1] - __uint_as_float(hi0 & 0xffff0000u));
         const uint32_t lo1 = pack_bf16(p[2] - __uint_as_float(hi1 << 16), p[3] - __uint_as_float(hi1 & 0xffff0000u));
@@ -268,8 +268,15 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
     }
-    // parameters of a span's values; gone: bit r: row r does not count
-    static __device__ __forceinline__ float load_pars(Pars& P, const unsigned char* st, int span, unsigned gone, int g)
+    // what the rows of a unit that `gone` names hold as values: with step and zero 0 it is 0
+    static __device__ __forceinline__ void clear(unsigned char* st, unsigned gone, int lane)
+    {
+        if ((gone >> lane) & 1u)
+#pragma unroll
+            for (int j = 0; j < GR; ++j) reinterpret_cast<uint32_t*>(st + Stage<D, true>::VP)[lane * GR + j] = 0u;
+    }
+    // parameters of a span's values
+    static __device__ __forceinline__ float load_pars(Pars& P, const unsigned char* st, int span, int g)
     {
         const unsigned char* pars = st + Stage<D, true>::VP + span * (64 * GR);
         float top = 0.f;
@@ -277,10 +284,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         for (int u = 0; u < 2; ++u) {
             get<Words>(P.p[u], pars + (rho(g) + 8 * u) * (4 * GR));
 #pragma unroll
-            for (int j = 0; j < GR; ++j) {
-                if (gone && ((gone >> (rho(g) + 8 * u)) & 1u)) P.p[u][j] = 0u;
-                top = fmaxf(top, par4_step(P.p[u][j]));
-            }
+            for (int j = 0; j < GR; ++j) top = fmaxf(top, par4_step(P.p[u][j]));
         }
         return top;
     }
@@ -296,7 +300,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int m = 0; m < MT; ++m) { A.a[m][0] *= f; A.a[m][1] *= f; A.a[m][2] *= f; A.a[m][3] *= f; }
     }
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, const unsigned char* st, int span, unsigned, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, const unsigned char* st, int span, int g, int t)
     {
         const unsigned char* values = st + Stage<D, true>::V + span * (8 * D);
         uint32_t v[4][(GR + 1) / 2];
@@ -384,32 +388,42 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     const int step = NW * nsplit, first = wid * nsplit + rank;
     unsigned char* const stage = s_dyn + wid * (STAGES * St::BYTES);
     const uint32_t stage_at = tc::smem_u32(stage);
-    // keys (values) and their parameters of unit i of the head into stage s
-    auto ask = [&](int i, int s, auto values) {
-        constexpr bool V = decltype(values)::value;
-        const int n_rows = rows.total - UR * i;
-        const uint32_t to = stage_at + s * St::BYTES + (V ? St::V : St::K) + 16 * lane;
-        const unsigned char* from = (V ? rows.V : rows.K) + (size_t)i * (UR * St::ROW) + 16 * lane;
-        auto copy = [&](auto whole) {
-            constexpr bool ALL = decltype(whole)::value;
+    // What is copied next of the keys (values): unit `unit` of the head, its rows and parameters from `row` and `par` on (this lane's 16 bytes).
+    struct Source { const unsigned char *row, *par; int unit; };
+    int units = (W + R + UR - 1) / UR, full = (W + R) / UR;    // of the head; whole ones
+    constexpr int P = UR * St::PAR;                            // bytes of a unit's key parameters
+    const bool par_lane = 16 * lane < P;
+    auto ask = [&](Source& S, uint32_t to, int par_to) {       // its next unit to `to`, the parameters `par_to` bytes behind
+        to += 16 * lane;
+        if (S.unit < full) {
+#pragma unroll
+            for (int u = 0; u < UR * St::ROW / 512; ++u) tc::cp_async16(to + 512 * u, S.row + 512 * u, 16);
+            if (FOUR && par_lane) tc::cp_async16(to + par_to, S.par, 16);
+        } else if (S.unit < units) {
+            const int n_rows = rows.total - UR * S.unit;
 #pragma unroll
             for (int u = 0; u < UR * St::ROW / 512; ++u)
-                if (ALL || 16 * lane + 512 * u < n_rows * St::ROW) tc::cp_async16(to + 512 * u, from + 512 * u, 16);
-            if constexpr (FOUR) {
-                constexpr int P = UR * St::PAR;                // (the last 16 bytes of a part of the cache are its own)
-                if ((P >= 512 || 16 * lane < P) && (ALL || 16 * lane < n_rows * St::PAR))
-                    tc::cp_async16(to + ((V ? St::VP : St::KP) - (V ? St::V : St::K)), (V ? rows.VP : rows.KP) + (size_t)i * P + 16 * lane, 16);
-            }
-        };
-        if (n_rows >= UR) copy(std::true_type());
-        else if (n_rows > 0) copy(std::false_type());
-        tc::cp_async_commit();                                 // (one group per call, whether there is anything to copy or not)
+                if (16 * lane + 512 * u < n_rows * St::ROW) tc::cp_async16(to + 512 * u, S.row + 512 * u, 16);
+            if (FOUR && par_lane && 16 * lane < n_rows * St::PAR) tc::cp_async16(to + par_to, S.par, 16);   // (the last 16 bytes of a part of the cache are its own)
+        }
+        S.unit += step;
+        S.row += (size_t)step * (UR * St::ROW);
+        S.par += (size_t)step * P;
     };
+    Source sk, sv;
+    auto ask_keys = [&](uint32_t to) { ask(sk, to + St::K, St::KP - St::K); };
+    auto ask_values = [&](uint32_t to) { ask(sv, to + St::V, St::VP - St::V); };
+    // bf16: keys and values are refilled as soon as each has been read, in copy groups of their own; 4 bits: together, which takes fewer instructions
+    constexpr int PENDING = FOUR ? STAGES - 1 : 2 * STAGES - 1;    // copy groups that may be on their way when the next one is waited for
     auto begin = [&]() {                                       // the first units of a pass
+        sk = {rows.K + (size_t)first * (UR * St::ROW) + 16 * lane, rows.KP + (size_t)first * P + 16 * lane, first};
+        sv = {rows.V + (size_t)first * (UR * St::ROW) + 16 * lane, rows.VP + (size_t)first * P + 16 * lane, first};
 #pragma unroll
         for (int b = 0; b < STAGES; ++b) {
-            ask(first + b * step, b, std::false_type());
-            ask(first + b * step, b, std::true_type());
+            ask_keys(stage_at + b * St::BYTES);
+            if (!FOUR) tc::cp_async_commit();
+            ask_values(stage_at + b * St::BYTES);
+            tc::cp_async_commit();
         }
     };
     begin();
@@ -431,7 +445,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     if (tid < D / 4) reinterpret_cast<uint4*>(s_kv)[tid] = reinterpret_cast<const uint4*>((tid < D / 8 ? k1 : v1) + (size_t)bh * D)[tid % (D / 8)];
     const int slot = n % W, p = n - W, half = rule.K / 2;
     rows.total = n < W ? n : W + cnt_old;
-    const int units = (rows.total + UR - 1) / UR, full = rows.total / UR;
+    units = (rows.total + UR - 1) / UR; full = rows.total / UR;
     const float zp = p >= 0 ? zc[slot] : 0.f;
     // Learned rule, the first block: logit of the newest token whose receptive field is complete.  A lane takes eight channels under a tap: a
     // word of the row's key or value codes, two runs of four weights.
@@ -594,27 +608,36 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
         int kept = 0;                                          // rows whose logits this warp has kept
 
-        int at_stage = 0;
+        const int ring_unit = masked_ring / UR, pool_unit = masked_pool / UR;
+        int at_stage = 0;                                      // in bytes
 #pragma unroll 1
         for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
-            const unsigned char* st = stage + at_stage * St::BYTES;
-            tc::cp_async_wait<2 * STAGES - 1>();
-            __syncwarp();                                      // every lane's copies of this unit's keys are there
+            unsigned char* st = stage + at_stage;
+            const uint32_t refill = stage_at + at_stage;
+            at_stage = at_stage == (STAGES - 1) * St::BYTES ? 0 : at_stage + St::BYTES;
+            tc::cp_async_wait<PENDING>();
+            __syncwarp();                                      // every lane's copies of this unit (bf16: of its keys) are there
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
-            __syncwarp();                                      // every lane has read the keys
-            ask(i + STAGES * step, at_stage, std::false_type());
-            unsigned gone = 0;                                 // rows of the unit that do not count
-            if (i >= full || i == masked_ring / UR || i == masked_pool / UR) {
-                if (i >= full) gone = ~0u << (rows.total - UR * i);
-                if (i == masked_ring / UR) gone |= 1u << (masked_ring % UR);
-                if (i == masked_pool / UR) gone |= 1u << (masked_pool % UR);
+            if (!FOUR) {
+                __syncwarp();                                  // every lane has read the keys
+                ask_keys(refill);
+                tc::cp_async_commit();
+                tc::cp_async_wait<PENDING>();
+                __syncwarp();                                  // ... every lane's copies of its values
+            }
+            if (i >= full || i == ring_unit || i == pool_unit) {
+                unsigned gone = i >= full ? ~0u << (rows.total - UR * i) : 0u;   // rows of the unit that do not count
+                if (i == ring_unit) gone |= 1u << (masked_ring % UR);
+                if (i == pool_unit) gone |= 1u << (masked_pool % UR);
 #pragma unroll
                 for (int x = 0; x < UNIT; ++x) {
                     if ((gone >> (16 * x + Gr::rho(g))) & 1u) c[x][0] = c[x][1] = -INFINITY;
                     if ((gone >> (16 * x + Gr::rho(g) + 8)) & 1u) c[x][2] = c[x][3] = -INFINITY;
                 }
+                Gr::clear(st, UR < 32 ? gone & ((1u << UR) - 1u) : gone, lane);
+                __syncwarp();
             }
             if constexpr (ACCUM) {                             // raw logits [query][row]
                 float* at = wlog + 2 * t * lpitch + kept + Gr::rho(g);
@@ -625,12 +648,10 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 }
                 kept += UR;
             }
-            tc::cp_async_wait<2 * STAGES - 1>();
-            __syncwarp();                                      // ... of its values
             typename Gr::Pars vpar[UNIT];
             float steps = 0.f;
 #pragma unroll
-            for (int x = 0; x < UNIT; ++x) steps = fmaxf(steps, Gr::load_pars(vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g));
+            for (int x = 0; x < UNIT; ++x) steps = fmaxf(steps, Gr::load_pars(vpar[x], st, x, g));
             // The reference m follows the maximum only when that has grown by 2^8 (weights stay below 2^8, in fp32): a vote per
             // unit instead of a reduction over its rows.
             float x0 = fmaxf(c[0][0], c[0][2]), x1 = fmaxf(c[0][1], c[0][3]);
@@ -657,10 +678,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3];
             }
 #pragma unroll
-            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, (gone >> (16 * x)) & 0xffffu, g, t);
-            __syncwarp();
-            ask(i + STAGES * step, at_stage, std::true_type());
-            at_stage = at_stage + 1 == STAGES ? 0 : at_stage + 1;
+            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, g, t);
+            __syncwarp();                                      // every lane has read the stage
+            if (FOUR) ask_keys(refill);
+            ask_values(refill);
+            tc::cp_async_commit();
         }
         tc::cp_async_wait<0>();                                // (units asked for before it was known how many rows are in use)
         __syncwarp();
