@@ -72,6 +72,14 @@ template <int D, bool FOUR> struct Stage {
     static_assert(ACC <= BYTES, "the outputs' place");
 };
 
+// N 4-byte words of shared memory (one load; from reinterpreted pointers the compiler makes single words)
+template <int N> __device__ __forceinline__ void lds(uint32_t (&x)[N], uint32_t at)
+{
+    if constexpr (N == 1) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(at));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(at));
+    else asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+}
+
 // The two products with a span of 16 rows that stands in shared memory, lane (g, t) = (lane / 4, lane % 4).  Rows past the last one and those that the
 // step leaves out have weight zero, and what they hold is cleared (zero times an infinite value is NaN).
 template <int D, bool SWZ, bool FOUR> struct Group;
@@ -82,7 +90,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     struct Query { uint4 f[KP]; float unit[2]; };              // pieces t, t + 4, .. of query g
     struct Acc { float a[MT][4]; };
     struct Pars {};
-    static __device__ __forceinline__ float load_pars(Pars&, const unsigned char*, int, int) { return 0.f; }
+    static __device__ __forceinline__ float load_pars(Pars&, uint32_t, int, int) { return 0.f; }
     static __device__ __forceinline__ bool too_large(const Acc&, float) { return false; }
     static __device__ __forceinline__ void lower(Acc&, float) {}
     static __device__ __forceinline__ int rho(int g) { return g; }
@@ -94,21 +102,21 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     }
     // c: rows g (0, 1) and g + 8 (2, 3), queries 2t and 2t + 1.  A product rounds its running sum towards zero, so every one starts from zero
     // and the parts are added to the nearest (see decode_mma.cu).  Lane (g, t) takes pieces t, t + 4, .. of rows g and g + 8.
-    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* st, int span, int g, int t)
+    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, uint32_t st, int span, int g, int t)
     {
-        uint4 k[2][KP];
+        uint32_t k[2][KP][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int j = 0; j < KP; ++j)
-                k[u][j] = *reinterpret_cast<const uint4*>(st + Stage<D, false>::K + (16 * span + g + 8 * u) * PITCH + (((t + 4 * j) ^ (SWZ ? g & 7 : 0)) << 4));
+                lds(k[u][j], st + g * PITCH + ((t ^ (SWZ ? g & 3 : 0)) << 4) + Stage<D, false>::K + (16 * span + 8 * u) * PITCH + ((4 * j) ^ (SWZ ? g & 4 : 0)) * 16);
         constexpr int NS = D == 128 ? 2 : 1;
         float cs[NS][4];
 #pragma unroll
         for (int i = 0; i < 2 * KP; ++i) {
             const int j = i >> 1, s = 2 * (i & 1);
             float part[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816(part, word(k[0][j], s), word(k[1][j], s), word(k[0][j], s + 1), word(k[1][j], s + 1), word(Q.f[j], s), word(Q.f[j], s + 1));
+            mma16816(part, k[0][j][s], k[1][j][s], k[0][j][s + 1], k[1][j][s + 1], word(Q.f[j], s), word(Q.f[j], s + 1));
 #pragma unroll
             for (int e = 0; e < 4; ++e) cs[i % NS][e] = i < NS ? part[e] : cs[i % NS][e] + part[e];
         }
@@ -138,22 +146,22 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
             if (lane < D / 8) *reinterpret_cast<uint4*>(st + Stage<D, false>::V + (__ffs(gone) - 1) * PITCH + 16 * lane) = make_uint4(0, 0, 0, 0);
     }
     // Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, const unsigned char* st, int span, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, uint32_t st, int span, int g, int t)
     {
         uint32_t v[4][VB];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int r = 2 * t + (u & 1) + 8 * (u >> 1);
-            const unsigned char* base = st + Stage<D, false>::V + (16 * span + r) * PITCH;
+            const uint32_t base = st + Stage<D, false>::V + (16 * span + r) * PITCH;
             if constexpr (D == 32) {
-                const uint2 x = *reinterpret_cast<const uint2*>(base + (g << 3));
-                v[u][0] = x.x; v[u][1] = x.y;
+                lds(v[u], base + (g << 3));
             } else {
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(base + (((g + 8 * j) ^ (SWZ ? r & 7 : 0)) << 4));
+                    uint32_t x[4];
+                    lds(x, base + (((g + 8 * j) ^ (SWZ ? r & 7 : 0)) << 4));
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) v[u][4 * j + w] = word(x, w);
+                    for (int w = 0; w < 4; ++w) v[u][4 * j + w] = x[w];
                 }
             }
         }
@@ -181,13 +189,6 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and inverse scales of queries 2t, 2t + 1
     struct Acc { float a[MT][4], z[GR][2], inv; };             // inv: the scale of P step
     struct Pars { uint32_t p[2][GR]; };                        // of rows rho(g), rho(g) + 8
-    template <typename U> static __device__ __forceinline__ void get(uint32_t (&x)[GR], const unsigned char* p)
-    {
-        const U u = *reinterpret_cast<const U*>(p);
-        memcpy(x, &u, sizeof(U));
-    }
-    using Words = std::conditional_t<GR == 1, uint32_t, std::conditional_t<GR == 2, uint2, uint4>>;
-    using Units = std::conditional_t<GR == 1, uint16_t, std::conditional_t<GR == 2, uint32_t, uint2>>;
     static __device__ __forceinline__ int rho(int g) { return (g >> 1) + 4 * (g & 1); }     // (g < 8)
     static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
     {
@@ -227,14 +228,14 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         Q.unit[0] = __shfl_sync(0xffffffffu, unit, 8 * t);
         Q.unit[1] = __shfl_sync(0xffffffffu, unit, 8 * t + 4);
     }
-    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, const unsigned char* st, int span, int g, int t)
+    static __device__ __forceinline__ void logits(float (&c)[4], const Query& Q, uint32_t st, int span, int g, int t)
     {
-        const unsigned char *keys = st + Stage<D, true>::K + span * (8 * D), *pars = st + Stage<D, true>::KP + span * (64 * GR);
+        const uint32_t keys = st + rho(g) * (D / 2) + t * (4 * GR), pars = st + rho(g) * (4 * GR);
         uint32_t k[2][GR], kp[2][GR];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            get<Words>(k[u], keys + (rho(g) + 8 * u) * (D / 2) + t * (4 * GR));
-            get<Words>(kp[u], pars + (rho(g) + 8 * u) * (4 * GR));
+            lds(k[u], keys + Stage<D, true>::K + (2 * span + u) * (4 * D));
+            lds(kp[u], pars + Stage<D, true>::KP + (2 * span + u) * (32 * GR));
         }
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
@@ -276,13 +277,12 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             for (int j = 0; j < GR; ++j) reinterpret_cast<uint32_t*>(st + Stage<D, true>::VP)[lane * GR + j] = 0u;
     }
     // parameters of a span's values
-    static __device__ __forceinline__ float load_pars(Pars& P, const unsigned char* st, int span, int g)
+    static __device__ __forceinline__ float load_pars(Pars& P, uint32_t st, int span, int g)
     {
-        const unsigned char* pars = st + Stage<D, true>::VP + span * (64 * GR);
         float top = 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            get<Words>(P.p[u], pars + (rho(g) + 8 * u) * (4 * GR));
+            lds(P.p[u], st + rho(g) * (4 * GR) + Stage<D, true>::VP + (2 * span + u) * (32 * GR));
 #pragma unroll
             for (int j = 0; j < GR; ++j) top = fmaxf(top, par4_step(P.p[u][j]));
         }
@@ -300,15 +300,19 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 #pragma unroll
         for (int m = 0; m < MT; ++m) { A.a[m][0] *= f; A.a[m][1] *= f; A.a[m][2] *= f; A.a[m][3] *= f; }
     }
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, const unsigned char* st, int span, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, uint32_t st, int span, int g, int t)
     {
-        const unsigned char* values = st + Stage<D, true>::V + span * (8 * D);
+        const uint32_t values = st + t * (D / 2) + g * (2 * GR) + Stage<D, true>::V + span * (8 * D);
         uint32_t v[4][(GR + 1) / 2];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const Units x = *reinterpret_cast<const Units*>(values + (t + 4 * u) * (D / 2) + g * (2 * GR));   // M-rows 2t + (u & 1) + 8 (u / 2)
-            if constexpr (GR == 1) v[u][0] = x;
-            else memcpy(v[u], &x, sizeof(x));
+            if constexpr (GR == 1) {                           // M-rows 2t + (u & 1) + 8 (u / 2)
+                uint16_t x;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(values + u * (2 * D)));
+                v[u][0] = x;
+            } else {
+                lds(v[u], values + u * (2 * D));
+            }
         }
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
@@ -613,8 +617,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 #pragma unroll 1
         for (int i = first; i < units; i += step) {
             float c[UNIT][4], p[UNIT][4];
-            unsigned char* st = stage + at_stage;
-            const uint32_t refill = stage_at + at_stage;
+            const uint32_t st = stage_at + at_stage;
             at_stage = at_stage == (STAGES - 1) * St::BYTES ? 0 : at_stage + St::BYTES;
             tc::cp_async_wait<PENDING>();
             __syncwarp();                                      // every lane's copies of this unit (bf16: of its keys) are there
@@ -622,7 +625,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             for (int x = 0; x < UNIT; ++x) Gr::logits(c[x], qf, st, x, g, t);
             if (!FOUR) {
                 __syncwarp();                                  // every lane has read the keys
-                ask_keys(refill);
+                ask_keys(st);
                 tc::cp_async_commit();
                 tc::cp_async_wait<PENDING>();
                 __syncwarp();                                  // ... every lane's copies of its values
@@ -636,7 +639,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                     if ((gone >> (16 * x + Gr::rho(g))) & 1u) c[x][0] = c[x][1] = -INFINITY;
                     if ((gone >> (16 * x + Gr::rho(g) + 8)) & 1u) c[x][2] = c[x][3] = -INFINITY;
                 }
-                Gr::clear(st, UR < 32 ? gone & ((1u << UR) - 1u) : gone, lane);
+                Gr::clear(stage + (st - stage_at), UR < 32 ? gone & ((1u << UR) - 1u) : gone, lane);
                 __syncwarp();
             }
             if constexpr (ACCUM) {                             // raw logits [query][row]
@@ -680,8 +683,8 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, g, t);
             __syncwarp();                                      // every lane has read the stage
-            if (FOUR) ask_keys(refill);
-            ask_values(refill);
+            if (FOUR) ask_keys(st);
+            ask_values(st);
             tc::cp_async_commit();
         }
         tc::cp_async_wait<0>();                                // (units asked for before it was known how many rows are in use)
