@@ -87,17 +87,23 @@ template <int D, bool SWZ, bool FOUR> struct Group;
 template <int D, bool SWZ> struct Group<D, SWZ, false> {
     static constexpr int KP = D / 32, VB = D / 16, PITCH = D * 2, MT = D / 16;
     static constexpr float LIFT = 1.f;
-    struct Query { uint4 f[KP]; float unit[2]; };              // pieces t, t + 4, .. of query g
+    struct Raw { uint4 u[KP]; };                               // pieces t, t + 4, .. of query g
+    struct Query { uint4 f[KP]; float unit[2]; };
     struct Acc { float a[MT][4]; };
     struct Pars {};
     static __device__ __forceinline__ float load_pars(Pars&, uint32_t, int, int) { return 0.f; }
     static __device__ __forceinline__ bool too_large(const Acc&, float) { return false; }
     static __device__ __forceinline__ void lower(Acc&, float) {}
     static __device__ __forceinline__ int rho(int g) { return g; }
-    static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
+    static __device__ __forceinline__ void load_q(Raw& r, const __nv_bfloat16* q, bool some, int g, int t)
     {
 #pragma unroll
-        for (int j = 0; j < KP; ++j) Q.f[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < KP; ++j) r.u[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D)[t + 4 * j] : make_uint4(0, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void set_q(Query& Q, const Raw& r, int)
+    {
+#pragma unroll
+        for (int j = 0; j < KP; ++j) Q.f[j] = r.u[j];
         Q.unit[0] = Q.unit[1] = 1.f;
     }
     // c: rows g (0, 1) and g + 8 (2, 3), queries 2t and 2t + 1.  A product rounds its running sum towards zero, so every one starts from zero
@@ -186,17 +192,22 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static constexpr int GR = D / kGroup4, MT = D / 16;
     static constexpr float LIFT = 16777216.f;                  // 2^24: logits are kept as sums of c 2^-24 q
+    struct Raw { uint4 u[GR]; };                               // channels 8t .. 8t + 7 of every group of query g
     struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and inverse scales of queries 2t, 2t + 1
     struct Acc { float a[MT][4], z[GR][2], inv; };             // inv: the scale of P step
     struct Pars { uint32_t p[2][GR]; };                        // of rows rho(g), rho(g) + 8
     static __device__ __forceinline__ int rho(int g) { return (g >> 1) + 4 * (g & 1); }     // (g < 8)
-    static __device__ __forceinline__ void load_q(Query& Q, const __nv_bfloat16* q, bool some, int g, int t)
+    static __device__ __forceinline__ void load_q(Raw& r, const __nv_bfloat16* q, bool some, int g, int t)
     {
-        uint4 u[GR];
+#pragma unroll
+        for (int j = 0; j < GR; ++j) r.u[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D + j * kGroup4)[t] : make_uint4(0, 0, 0, 0);
+    }
+    static __device__ __forceinline__ void set_q(Query& Q, const Raw& r, int t)
+    {
+        const uint4 (&u)[GR] = r.u;
         float top = 0.f;
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
-            u[j] = some ? reinterpret_cast<const uint4*>(q + (size_t)g * D + j * kGroup4)[t] : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(word(u[j], w) << 16)), fabsf(__uint_as_float(word(u[j], w) & 0xffff0000u))));
         }
@@ -385,7 +396,23 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     pdl_launch_dependents();
     pdl_wait();
 
-    // Everything whose address is known is asked for at once: the rows that a warp begins with too, whether or not they turn out to be in use.
+    // What is small and waited for first is asked for first; then the rows that a warp begins with, whether or not they turn out to be in use (behind
+    // them the counters took two thousand cycles); then what needs the counters, and the rest of the stages.
+    const int n_held = meta[0], cnt_held = meta[1];
+    typename Gr::Raw q_raw;
+    Gr::load_q(q_raw, q1 + (size_t)bh * G * D, g < G, g, t);
+    constexpr int PRE = NT < 256 ? 4 : 2;                      // scores and positions of the pool, before it is known whether the decision needs them
+    // A pool that the cluster's blocks would each take several rounds to look through they look through together, which costs a meeting.
+    const bool share_scan = shared_head && R > 4 * PRE * NT;
+    const int part = share_scan ? (R + nsplit - 1) / nsplit : R, pre0 = share_scan ? rank * part : 0, pre1 = min(R, pre0 + part);
+    float pz[PRE];
+    int pp[PRE];
+#pragma unroll
+    for (int u = 0; u < PRE; ++u) {
+        const int m = pre0 + tid + u * NT;
+        pz[u] = m < pre1 ? zc[W + m] : INFINITY;
+        pp[u] = m < pre1 ? pidx[m] : -1;
+    }
     Rows rows;
     rows.K = blk + L.off_k; rows.V = blk + L.off_v; rows.KP = blk + L.off_kp; rows.VP = blk + L.off_vp;
     rows.total = W + R;
@@ -419,33 +446,21 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     auto ask_values = [&](uint32_t to) { ask(sv, to + St::V, St::VP - St::V); };
     // bf16: keys and values are refilled as soon as each has been read, in copy groups of their own; 4 bits: together, which takes fewer instructions
     constexpr int PENDING = FOUR ? STAGES - 1 : 2 * STAGES - 1;    // copy groups that may be on their way when the next one is waited for
-    auto begin = [&]() {                                       // the first units of a pass
+    auto fill = [&](int s) {                                   // the next unit into stage s
+        ask_keys(stage_at + s * St::BYTES);
+        if (!FOUR) tc::cp_async_commit();
+        ask_values(stage_at + s * St::BYTES);
+        tc::cp_async_commit();
+    };
+    auto begin = [&]() {                                       // the first unit of a pass
         sk = {rows.K + (size_t)first * (UR * St::ROW) + 16 * lane, rows.KP + (size_t)first * P + 16 * lane, first};
         sv = {rows.V + (size_t)first * (UR * St::ROW) + 16 * lane, rows.VP + (size_t)first * P + 16 * lane, first};
-#pragma unroll
-        for (int b = 0; b < STAGES; ++b) {
-            ask_keys(stage_at + b * St::BYTES);
-            if (!FOUR) tc::cp_async_commit();
-            ask_values(stage_at + b * St::BYTES);
-            tc::cp_async_commit();
-        }
+        fill(0);
     };
     begin();
-    const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R);
+    const int n = max(n_held, 0), cnt_old = min(max(cnt_held, 0), R);
     typename Gr::Query qf;
-    Gr::load_q(qf, q1 + (size_t)bh * G * D, g < G, g, t);
-    constexpr int PRE = NT < 256 ? 4 : 2;                      // scores and positions of the pool, before it is known whether the decision needs them
-    // A pool that the cluster's blocks would each take several rounds to look through they look through together, which costs a meeting.
-    const bool share_scan = shared_head && R > 4 * PRE * NT;
-    const int part = share_scan ? (R + nsplit - 1) / nsplit : R, pre0 = share_scan ? rank * part : 0, pre1 = min(R, pre0 + part);
-    float pz[PRE];
-    int pp[PRE];
-#pragma unroll
-    for (int u = 0; u < PRE; ++u) {
-        const int m = pre0 + tid + u * NT;
-        pz[u] = m < pre1 ? zc[W + m] : INFINITY;
-        pp[u] = m < pre1 ? pidx[m] : -1;
-    }
+    Gr::set_q(qf, q_raw, t);
     if (tid < D / 4) reinterpret_cast<uint4*>(s_kv)[tid] = reinterpret_cast<const uint4*>((tid < D / 8 ? k1 : v1) + (size_t)bh * D)[tid % (D / 8)];
     const int slot = n % W, p = n - W, half = rule.K / 2;
     rows.total = n < W ? n : W + cnt_old;
@@ -495,6 +510,9 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 tap_new += w[lane + 32 * c] * __bfloat162float(k1[(size_t)bh * D + lane + 32 * c]) + w[D + lane + 32 * c] * __bfloat162float(v1[(size_t)bh * D + lane + 32 * c]);
         }
     }
+
+#pragma unroll
+    for (int s = 1; s < STAGES; ++s) fill(s);
 
     // ---- what happens to the token leaving the window ------------------------------------------------------------
     int dst = -1, cnt_new = cnt_old;
@@ -591,9 +609,12 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     for (int g0 = 0; g0 < G; g0 += MQ) {
         const int nq = min(MQ, G - g0);
         if (g0 > 0) {                                          // further query heads read the rows again
-            Gr::load_q(qf, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
+            Gr::load_q(q_raw, q1 + ((size_t)bh * G + g0) * D, g < nq, g, t);
             __syncthreads();                                   // the previous pass's outputs, which stand in the stages, have been combined
             begin();
+#pragma unroll
+            for (int s = 1; s < STAGES; ++s) fill(s);
+            Gr::set_q(qf, q_raw, t);
         }
         if (rank == 0)                                         // the incoming token's logits
             for (int u = wid; u < nq; u += NW) {
