@@ -68,9 +68,9 @@ __device__ __forceinline__ uint32_t code4(float x, uint32_t par)
     if (!(step > 0.f)) return 0u;
     return (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(x - par4_zero(par), step)), 0.f), 15.f);
 }
-// The codes of eight channels, the first in the lowest nibble.  The quotient d / step, d = x - zero, comes from the reciprocal y of step by one
-// correction, q + (d - q step) y (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990): a rounding of the
-// exact quotient moved by less than 2 units of its last place times 2^-24.  That rounds to the same code as the correctly rounded quotient: an
+// The codes of eight channels, the first in the lowest nibble.  The quotient d / step, d = x - zero, comes from the reciprocal y of step (the
+// instruction's, within 2^-23) by one correction, q + (d - q step) y (Markstein, Computation of elementary functions on the IBM RISC System/6000
+// processor, 1990): a rounding of the exact quotient moved by less than 4 units of its last place times 2^-23.  That rounds to the same code as the correctly rounded quotient: an
 // exact half k + 1/2 stays one (bf16 rows have them all the time), and the two could part only where the quotient is that close to the border
 // between k + 1/2 and its neighbour, a number of 25 bits, which times step is no fp32 number d (step has 8 bits, so that what is not on
 // the border is further off).  Rounding is by adding 1.5 2^23, which leaves the code in the lowest bits.  Steps outside 2^-100 .. 2^100, where
@@ -80,7 +80,9 @@ template <bool EXACT> __device__ __forceinline__ uint32_t codes4(const float (&f
 {
     constexpr float MAGIC = 12582912.f;
     constexpr uint32_t REST = 0x4b400000u * 0x11111111u;       // (modulo 2^32: what the bits above the codes add up to)
-    const float step = par4_step(par), zero = par4_zero(par), y = __frcp_rn(step);
+    const float step = par4_step(par), zero = par4_zero(par);
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(step));
     uint32_t w = 0u;
     if (step > 0x1p-100f && step < 0x1p100f) {
         w = 0u - REST;
@@ -112,7 +114,11 @@ __device__ __forceinline__ uint32_t group4_of(const uint4& u)     // bf16
         const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&x), o);
         x = __hmin2_nan(x, bf(other));
     }
-    return group4(__bfloat162float(x.x), -__bfloat162float(x.y), false);
+    // (as group4, with the minimum's bits as they are)
+    const float step = (-__bfloat162float(x.y) - __bfloat162float(x.x)) * (1.f / 15.f);
+    const __nv_bfloat162 par = __floats2bfloat162_rn(step, __bfloat162float(x.x));
+    const uint32_t p = *reinterpret_cast<const uint32_t*>(&par);
+    return (p & 0x7f80u) == 0x7f80u || (p & 0x7f800000u) == 0x7f800000u ? 0x7fc07fc0u : p;
 }
 __device__ __forceinline__ uint32_t group4_of(const float (&f)[8])
 {
