@@ -3,8 +3,8 @@
 // Bound by memory and, for the rounding, nearly as much by instructions: a thread takes eight channels of the key and of the value of ROWS rows (16
 // or 32 bytes each), four threads a group; they meet in two shuffles for its extremes.  Scores, positions and counters are copied by the same
 // blocks.
-// Measured (B200, 256 heads x 1,280 rows, d = 64, bf16; 84 MB and 27 MB, 17.4 us at 6.56 TB/s): pack 32.5 us, of which instructions take about 27 (165 per
-// eight channels; with a division per channel it took 70), unpack 22.9 us.
+// Measured (B200, 256 heads x 1,280 rows, d = 64, bf16; 84 MB and 27 MB, 17.4 us at 6.56 TB/s): pack 30.7 us, of which instructions take about 25 (150
+// per eight channels; with a division per channel it took 70), unpack 22.6 us.
 #include <type_traits>
 
 #include "cache4.cuh"

@@ -2,13 +2,14 @@
 // operands, as in decode_mma.cu, every query head of a group at once, heads split over warps and clusters where there are few.
 //
 // Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there the instructions that unpack and weigh them count for more
-// (about 230 per 16 rows at d = 64, of which the two products' operands are 80, and 2,000 a warp beside them, at 0.55 per cycle: 14 warps an SM do not
+// (about 190 per 16 rows at d = 64, of which the two products' operands are 60, and 2,000 a warp beside them, at 0.55 per cycle: 14 warps an SM do not
 // hide their latencies, and registers for more are not there).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
 // through stages of its own in shared memory, keeps its own reference, sum and output, and meets the others once at the end.  The incoming token
 // is no row: its logit is a dot product on the fp32 ALUs, and it joins where the warps meet.
 //
 // Scores (accumulated attention): a row's weight needs the sum over all rows, so the raw logits of a warp's rows stay in shared memory until the
-// blocks have met; then every warp adds its rows' weights, summed over the query heads, to their scores.  One read and one write of 4 bytes a row.
+// blocks have met (or, where they do not fit, come from the keys once more); then every warp adds its rows' weights, summed over the query heads, to
+// their scores.  One read and one write of 4 bytes a row.
 //
 // Products are mma.sync m16n8k16: logits S^T[16 rows][8 queries] = K q^T, output O^T[16 channels][8 queries] += V^T P^T, N = 8 queries.
 // Rows in 4 bits.  A code is an fp16 number as it stands: the low ten bits of a half are its fraction, so that c in bits 0-3 is the subnormal number
@@ -24,15 +25,15 @@
 //
 // Measured (B200, us a step in a CUDA graph of steps over three caches in turn, full pools; bytes that cannot be avoided at 6.56 TB/s):
 //                                                    accumulated, bf16    4 bits, accumulated    4 bits, learned
-//   2,048 heads x 256 rows, d = 64                       28.5 (21.5)          21.7 (7.2)            20.9 (6.7)
-//   256 x 1,280, four query heads each, d = 64           22.0 (13.3)          15.5 (4.5)            14.2 (4.2)
-//   2,048 x 1,024, d = 64                                 107 (85.3)          66.5 (28.8)           58.3 (26.9)
-//   512 x 1,024, d = 128                                 48.5 (41.9)          30.7 (13.6)
-//   8 x 17,408, four query heads each, d = 128           30.9 (11.1)          24.1 (3.7)            19.9 (3.6)
-//   16 x 1,024, d = 128 (one user)                        9.3 (1.3)            8.8 (0.4)             8.2 (0.4)
-// Of a step about 5 us are the chain of launch, counters, first rows, meeting and write-back (32 rows a head: 5.1 to 8).  What did not help: 4-bit
+//   2,048 heads x 256 rows, d = 64                       27.7 (21.5)          19.4 (7.2)            19.2 (6.7)
+//   256 x 1,280, four query heads each, d = 64           20.3 (13.3)          14.7 (4.5)            12.8 (4.2)
+//   2,048 x 1,024, d = 64                                 108 (85.3)          58.8 (28.8)           51.9 (26.9)
+//   512 x 1,024, d = 128                                 47.4 (41.9)          28.8 (13.6)
+//   8 x 17,408, four query heads each, d = 128           29.3 (11.1)          23.0 (3.7)            18.4 (3.6)
+//   16 x 1,024, d = 128 (one user)                        9.0 (1.3)            8.4 (0.4)             7.9 (0.4)
+// Of a step 5 to 8 us are the chain of launch, counters, first rows, meeting and write-back (what 32 rows a head take).  What did not help: 4-bit
 // rows in 80 registers and 24 warps an SM (2,048 x 256: 27.8), bulk copies with a barrier per stage in the place of 16-byte ones (the same for bf16,
-// and 35 instructions per 16 rows more), codes as bf16 numbers 16 + c with P in two terms (1.05 us per 16 rows of 2,048 heads, now 0.72).
+// and 35 instructions per 16 rows more), codes as bf16 numbers 16 + c with P in two terms (1.05 us per 16 rows of 2,048 heads, now 0.67).
 #pragma once
 #include <cfloat>
 #include <cooperative_groups.h>
@@ -360,13 +361,17 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static __device__ __forceinline__ int channel(int m, int g) { return (m >> 1) * kGroup4 + 4 * g + 2 * (m & 1); }
 };
 
-template <int D, int NW, int STAGES, bool SWZ, bool FOUR, bool ACCUM>
+// Where the weights of accumulated attention come from: logits kept in shared memory, or the keys once more (see launch_rows_mma).
+enum { LEARNED = 0, KEPT = 1, AGAIN = 2 };
+
+template <int D, int NW, int STAGES, bool SWZ, bool FOUR, int RULE>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
     float scale, int G, int most)                              // most: rows whose logits a warp may have to keep (whole units)
 {
     using Gr = Group<D, SWZ, FOUR>;
+    constexpr bool ACCUM = RULE != LEARNED;
     constexpr int NT = NW * 32, MT = D / 16, PITCH = D + 8, CPL = D / 32, GR = D / kGroup4;
     using St = Stage<D, FOUR>;
     constexpr int UR = St::UR, UNIT = UR / 16;
@@ -663,7 +668,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 Gr::clear(stage + (st - stage_at), UR < 32 ? gone & ((1u << UR) - 1u) : gone, lane);
                 __syncwarp();
             }
-            if constexpr (ACCUM) {                             // raw logits [query][row]
+            if constexpr (RULE == KEPT) {                      // raw logits [query][row]
                 float* at = wlog + 2 * t * lpitch + kept + Gr::rho(g);
 #pragma unroll
                 for (int x = 0; x < UNIT; ++x) {
@@ -727,7 +732,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 old[b] = e < kept && counts(row) ? row == slot && p >= 0 ? zp : zc[row] : 0.f;   // (the popped row's place may already have been written)
             }
         };
-        if (ACCUM && last) load_old(lane);
+        if (RULE == KEPT && last) load_old(lane);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
         Gr::finish(acc);
@@ -787,7 +792,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 if (e0 + lane < per) o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * inv);
             }
         }
-        if constexpr (ACCUM) {
+        if constexpr (RULE == KEPT) {
             // ---- weights of this warp's rows into their scores.  Every block has read the old ones that its decision needs.
             for (int base = 0; base < kept; base += 32 * BATCH) {   // (the same in the whole warp)
                 const int e0 = base + lane;
@@ -810,6 +815,52 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 }
             }
             __syncwarp();                                      // (the next pass writes logits where these were)
+        }
+        if constexpr (RULE == AGAIN) {
+            // ---- the same from the keys, which are read once more.  Lane (g, t) has the logits of rows rho(g), + 8 (+ 16, + 24) for two queries; the four
+            // lanes of a g add them up, and lane t is left with row rho(g) + 8 t.  The passes add to the scores in the order of the query heads.
+            __syncthreads();                                   // the outputs, which stand in the stages, have been combined
+            const float ma = __shfl_sync(0xffffffffu, qm, 2 * t), mb = __shfl_sync(0xffffffffu, qm, 2 * t + 1);
+            const float wa = __shfl_sync(0xffffffffu, qi, 2 * t), wb = __shfl_sync(0xffffffffu, qi, 2 * t + 1);
+            sk = {rows.K + (size_t)first * (UR * St::ROW) + 16 * lane, rows.KP + (size_t)first * P + 16 * lane, first};
+#pragma unroll
+            for (int s = 0; s < STAGES; ++s) { ask_keys(stage_at + s * St::BYTES); tc::cp_async_commit(); }
+            int at_stage = 0;
+#pragma unroll 1
+            for (int i = first; i < units; i += step) {
+                const uint32_t st = stage_at + at_stage;
+                at_stage = at_stage == (STAGES - 1) * St::BYTES ? 0 : at_stage + St::BYTES;
+                const int row = UR * i + Gr::rho(g) + 8 * t;
+                const bool mine = t < 2 * UNIT && counts(row), leaves = row == slot && p >= 0;
+                float* const to = zc + (leaves ? W + dst : row);
+                // (the popped row's place may already have the incoming token's score)
+                const float before = !mine ? 0.f : g0 > 0 ? *to : rule.decay > 0.f ? rule.decay * (leaves ? zp : *to) : 0.f;
+                tc::cp_async_wait<STAGES - 1>();
+                __syncwarp();
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int u = 0; u < UNIT; ++u) {
+                    float c[4];
+                    Gr::logits(c, qf, st, u, g, t);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float a = 2 * t < nq ? exp2_fast(fmaf(c[2 * e], Gr::LIFT, -ma) * sq0) * wa : 0.f;
+                        x[2 * u + e] = 2 * t + 1 < nq ? fmaf(exp2_fast(fmaf(c[2 * e + 1], Gr::LIFT, -mb) * sq1), wb, a) : a;
+                    }
+                }
+                __syncwarp();                                  // every lane has read the stage
+                ask_keys(st);
+                tc::cp_async_commit();
+                const bool odd = t & 1, high = t & 2;
+                const float y0 = (odd ? x[1] : x[0]) + __shfl_xor_sync(0xffffffffu, odd ? x[0] : x[1], 1);
+                const float y1 = (odd ? x[3] : x[2]) + __shfl_xor_sync(0xffffffffu, odd ? x[2] : x[3], 1);
+                const float z = (high ? y1 : y0) + __shfl_xor_sync(0xffffffffu, high ? y0 : y1, 2);
+                if (mine) *to = before + z;
+            }
+            tc::cp_async_wait<0>();
+            __syncwarp();
+        }
+        if constexpr (ACCUM) {
             if (rank == 0 && wid == 0) {
                 float a = lane < nq ? exp2_fast((s_new[lane] - qm) * qs) * qi : 0.f;
                 a = warp_sum(a);
@@ -818,7 +869,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         }
     }
 
-    // ---- write-back: only what changed; every read of the old block lies before the barriers above ------------------
+    // ---- write-back: only what changed; every read of the old block lies before the barriers above and here ------------------
+    if (RULE == AGAIN) {                                       // (the keys of the rows that are written now have been read a second time)
+        if (shared_head) cluster.sync();
+        else __syncthreads();
+    }
     if (rank != 0) return;
     if (dst >= 0)
 #pragma unroll
@@ -856,8 +911,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     }
 }
 
-// How many warps share a head: all warps of the launch are resident at once where that is possible, as in decode_mma.cu.  Under accumulated
-// attention a block's logits have to fit beside those of the SM's other blocks.
+// How many warps share a head: all warps of the launch are resident at once where that is possible, as in decode_mma.cu.
 template <bool FOUR, bool ACCUM>
 int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1,
                     void* o1, float* lse1, cudaStream_t st)
@@ -866,9 +920,6 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     if (int e = device_sm_count(&n_sm)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm;
     const int UR = FOUR || p.d < 128 ? 32 : 16;                // rows that a warp takes at a time (Stage::UR)
-    const int kept = ACCUM ? (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0) : 0;   // floats per row in shared memory
-    auto most = [&](int all) { return ((rows + UR - 1) / UR + all - 1) / all * UR; };   // rows of a warp at most, `all` of which share the head
-    auto smem = [&](int nw, int split) { return (size_t)nw * (most(nw * split) + 4) * kept * 4; };   // of logits
     // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, take 39.5 us with four warps,
     // 30.9 with eight (bf16; 4-bit blocks of eight take an SM's registers: 24.1 and 33.0).  16 heads x 1,024 rows take 7.9 us with four warps in
     // clusters of 8 and 13.1 with eight (4 bits, d = 128).  Clusters of 16 only where each block has an SM to itself: 16 heads took as long as 32.
@@ -876,14 +927,29 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     const int most_w = p.d == 128 && (FOUR || !is_long) ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
     int nw = 1, nsplit = 1;
     for (int c : {2, 4, 8})
-        if (c <= most_w && ((BH <= n_sm * (wps / c) && rows / c >= 16) || smem(c / 2, 1) * (wps / (c / 2)) > 96 * 1024)) nw = c;
+        if (c <= most_w && BH <= n_sm * (wps / c) && rows / c >= 16) nw = c;
     if (nw == most_w)
-        while (nsplit < most_split && ((BH * nw * nsplit * 2 <= (nsplit < 8 ? warps : warps / 2) && rows / (nw * nsplit * 2) >= 8) || smem(nw, nsplit) > 64 * 1024)) nsplit *= 2;
+        while (nsplit < most_split && BH * nw * nsplit * 2 <= (nsplit < 8 ? warps : warps / 2) && rows / (nw * nsplit * 2) >= 8) nsplit *= 2;
+    // Accumulated attention: the logits stay in shared memory while those of the blocks that share an SM fit beside their stages.  Where they do not,
+    // the keys are read once more: their half of the bytes (of which L2 has some) and of the instructions.  For bf16 rows, whose bytes count, more
+    // blocks a head with fewer logits each come first, if no SM then has fewer warps and it takes at most two rounds.  Kept in more blocks | again:
+    //   bf16    256 heads x 4,024 rows, 4 query heads, d = 64     59.9 | 66.7 us     64 x 17,408, 4, d = 128   113 | 139      64 x 8,192, 8, d = 128   65 | 71
+    //           256 x 2,816, 8, d = 64 (half the warps)           73.3 | 48.6        512 x 2,048, 8, d = 64 (3.5 rounds)      81 | 70
+    //   4 bits  256 x 2,816, 8, d = 64     39.8 | 32.8     the same at d = 128     113 | 51     256 x 4,024, 4     44 | 43     64 x 17,408, 4, d = 128    77 | 85
+    const int kept = (p.G < MQ ? p.G : MQ) + (p.G > MQ ? 1 : 0);               // floats per row
+    auto smem = [&](int w, int split) { return (size_t)w * (((rows + UR - 1) / UR + w * split - 1) / (w * split) * UR + 4) * kept * 4; };
+    bool keep = smem(nw, nsplit) * (size_t)fmax(1., fmin(wps / nw, ((double)BH * nsplit + n_sm - 1) / n_sm)) <= 96 * 1024;
+    if (!FOUR && ACCUM && !keep) {
+        int more = nsplit;
+        while (more < MAX_SPLIT && smem(most_w, more) > 64 * 1024) more *= 2;
+        const size_t block = smem(most_w, more) + (size_t)most_w * 8 * 1024 + 12 * 1024;   // with its stages (8 KB a warp)
+        if (block * (wps / most_w) <= 224 * 1024 && (long long)BH * more <= 2ll * n_sm * (wps / most_w)) { keep = true; nw = most_w; nsplit = more; }
+    }
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
-        auto with = [&](auto stages) {
-            constexpr int STAGES = decltype(stages)::value;
-            auto kern = decode_rows_mma_kernel<D, NW, STAGES, decltype(s)::value, FOUR, ACCUM>;
+        auto with_kind = [&](auto stages, auto kind) {
+            constexpr int STAGES = decltype(stages)::value, RULE = decltype(kind)::value;
+            auto kern = decode_rows_mma_kernel<D, NW, STAGES, decltype(s)::value, FOUR, RULE>;
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -908,13 +974,17 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
                     return (int)LTE_OK; })) return e;
             const int split = nsplit < split_most ? nsplit : split_most;
             cfg.gridDim = dim3(BH * split); cfg.blockDim = dim3(NW * 32); cfg.stream = st;
-            cfg.dynamicSmemBytes = smem(nw, split) + NW * STAGES * Stage<D, FOUR>::BYTES;
+            cfg.dynamicSmemBytes = (RULE == KEPT ? smem(nw, split) : 0) + NW * STAGES * Stage<D, FOUR>::BYTES;
             if (cfg.dynamicSmemBytes > kMostSmem) return (int)LTE_ERR_UNSUPPORTED;
             attr[1].val.clusterDim.x = split;
             cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
             return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
                                                   (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
-                                                  most(nw * split)));
+                                                  ((rows + UR - 1) / UR + nw * split - 1) / (nw * split) * UR));
+        };
+        auto with = [&](auto stages) {
+            if constexpr (!ACCUM) return with_kind(stages, std::integral_constant<int, LEARNED>());
+            else return keep ? with_kind(stages, std::integral_constant<int, KEPT>()) : with_kind(stages, std::integral_constant<int, AGAIN>());
         };
         // two stages a warp; three where eight warps of an SM have the room, one where 16 have not (bf16 at d = 128: 8 KB a stage), unless few
         // heads leave it (16 x 1,024 rows: 9.7 us with one, 9.3 with two)

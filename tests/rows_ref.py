@@ -34,16 +34,16 @@ class Layout:
             off = up(off + size, align)
         self.stride = up(off, 256)
 
-    def part(self, cache, name, dtype):
+    def part(self, cache, name, dtype, heads=slice(None)):
         a, b = self.at[name]
-        return cache[256:].view(-1, self.stride)[:, a:b].contiguous().view(dtype)
+        return cache[256:].view(-1, self.stride)[heads, a:b].contiguous().view(dtype)
 
-    def rows_of(self, cache, name):
+    def rows_of(self, cache, name, heads=slice(None)):
         """Keys or values as the cache holds them: float64 [heads, W + R, d]."""
         s = self.s
         if self.four:
-            b = self.part(cache, name, torch.uint8).cpu().numpy().reshape(-1, self.rows, s.d // 2)
-            par = self.part(cache, name + "par", torch.bfloat16).double().cpu().numpy().reshape(-1, self.rows, s.d // 32, 2)
+            b = self.part(cache, name, torch.uint8, heads).cpu().numpy().reshape(-1, self.rows, s.d // 2)
+            par = self.part(cache, name + "par", torch.bfloat16, heads).double().cpu().numpy().reshape(-1, self.rows, s.d // 32, 2)
             out = np.empty((b.shape[0], self.rows, s.d))
             per = 8 if name == "k" else 4
             for x in range(s.d):                               # nibble x of a row
@@ -52,7 +52,7 @@ class Layout:
                 code = (b[..., x // 2] >> (4 * (x % 2))) & 15
                 out[..., g * 32 + t * per + i] = par[..., g, 1] + code * par[..., g, 0]
             return out
-        x = self.part(cache, name, torch.bfloat16 if self.esz == 2 else torch.float32).double().cpu().numpy()
+        x = self.part(cache, name, torch.bfloat16 if self.esz == 2 else torch.float32, heads).double().cpu().numpy()
         x = x.reshape(x.shape[0], -1, s.d)
         if self.swizzled:
             y = np.empty_like(x)
@@ -62,11 +62,11 @@ class Layout:
             x = y
         return x[:, :self.rows]
 
-    def state(self, cache):
-        return {"k": self.rows_of(cache, "k"), "v": self.rows_of(cache, "v"),
-                "score": self.part(cache, "score", torch.float32).double().cpu().numpy(),
-                "pos": self.part(cache, "pos", torch.int32).cpu().numpy().astype(np.int64).reshape(self.s.B * self.s.H, self.s.R),
-                "count": self.part(cache, "count", torch.int32).cpu().numpy().astype(np.int64)}
+    def state(self, cache, heads=slice(None)):
+        count = self.part(cache, "count", torch.int32, heads).cpu().numpy().astype(np.int64)
+        return {"k": self.rows_of(cache, "k", heads), "v": self.rows_of(cache, "v", heads),
+                "score": self.part(cache, "score", torch.float32, heads).double().cpu().numpy(),
+                "pos": self.part(cache, "pos", torch.int32, heads).cpu().numpy().astype(np.int64).reshape(len(count), self.s.R), "count": count}
 
 
 def four(x):
@@ -85,10 +85,12 @@ def four(x):
     return val.reshape(x.shape), per(step), per(zero)
 
 
-def step(s, lay, before, q1, k1, v1, accum, decay=1.0, w=None, bias=None):
-    """State after one step, o, lse in 64 bits, and bounds of the error of each: {"o", "lse", "score"}."""
+def step(s, lay, before, q1, k1, v1, accum, decay=1.0, w=None, bias=None, which=None):
+    """State after one step, o, lse in 64 bits, and bounds of the error of each: {"o", "lse", "score"}.  which: the heads that `before`, q1, k1, v1
+    are of (all)."""
     st = {n: a.copy() for n, a in before.items()}
-    heads, W, R, d, G = s.B * s.H, s.W, s.R, s.d, max(1, s.group)
+    which = list(range(s.B * s.H)) if which is None else which
+    heads, W, R, d, G = len(which), s.W, s.R, s.d, max(1, s.group)
     scale = s.softmax_scale if s.softmax_scale > 0 else 1.0 / np.sqrt(d)
     f = lambda t: t.double().cpu().numpy()  # noqa: E731
     q, kn, vn = f(q1).reshape(heads, G, d), f(k1).reshape(heads, d), f(v1).reshape(heads, d)
@@ -154,13 +156,13 @@ def step(s, lay, before, q1, k1, v1, accum, decay=1.0, w=None, bias=None):
             taps = w.shape[1]
             j = n - taps // 2
             if j >= 0:
-                z, mag = 0.0 if bias is None else float(bias[h % s.H]), 0.0
+                z, mag, hw = 0.0 if bias is None else float(bias[which[h] % s.H]), 0.0, which[h] % s.H
                 for t in range(taps):
                     tok = j + t - taps // 2
                     if tok >= 0:
                         kr, vr = (kn[h], vn[h]) if tok == n else (before["k"][h, tok % W], before["v"][h, tok % W])
-                        z += w[h % s.H, t, :d] @ kr + w[h % s.H, t, d:] @ vr
-                        mag += np.abs(w[h % s.H, t, :d]) @ np.abs(kr) + np.abs(w[h % s.H, t, d:]) @ np.abs(vr)
+                        z += w[hw, t, :d] @ kr + w[hw, t, d:] @ vr
+                        mag += np.abs(w[hw, t, :d]) @ np.abs(kr) + np.abs(w[hw, t, d:]) @ np.abs(vr)
                 st["score"][h, j % W] = z
                 bound["score"][h, j % W] = EPS * (2 * d * taps + taps + 2) * (mag + abs(z))
         if taken >= 0:
@@ -171,28 +173,30 @@ def step(s, lay, before, q1, k1, v1, accum, decay=1.0, w=None, bias=None):
     return st, o, lse, bound
 
 
-def magnitudes(lay, cache, state):
+def magnitudes(lay, cache, state, heads=slice(None)):
     """48 step + |zero| of every channel of a cache in 4 bits, for the bounds."""
     for name in ("k", "v"):
-        par = lay.part(cache, name + "par", torch.bfloat16).double().cpu().numpy().reshape(-1, lay.rows, lay.s.d // 32, 2)
+        par = lay.part(cache, name + "par", torch.bfloat16, heads).double().cpu().numpy().reshape(-1, lay.rows, lay.s.d // 32, 2)
         state[name + "mag"] = np.repeat(48 * par[..., 0] + np.abs(par[..., 1]), 32, axis=-1)
     return state
 
 
-def check_step(s, lay, cache, q1, k1, v1, call, accum, decay=1.0, w=None, bias=None):
-    """Runs `call` on the cache and holds what it leaves to the step in 64 bits.  Returns o, lse of the call."""
-    before = lay.state(cache)
+def check_step(s, lay, cache, q1, k1, v1, call, accum, decay=1.0, w=None, bias=None, which=None):
+    """Runs `call` on the cache and holds what it leaves (in the heads `which`) to the step in 64 bits.  Returns o, lse of the call."""
+    heads = slice(None) if which is None else torch.tensor(which, device=cache.device)
+    of = lambda t, d: t.reshape(s.B * s.H, -1, d)[heads]  # noqa: E731
+    before = lay.state(cache, heads)
     if lay.four:
-        magnitudes(lay, cache, before)
-    want, o64, l64, bound = step(s, lay, before, q1, k1, v1, accum, decay, w, bias)
+        magnitudes(lay, cache, before, heads)
+    want, o64, l64, bound = step(s, lay, before, of(q1, s.d), of(k1, s.d), of(v1, s.d), accum, decay, w, bias, which)
     o, lse = call()
     torch.cuda.synchronize()
-    after = lay.state(cache)
+    after = lay.state(cache, heads)
     assert np.array_equal(after["count"], want["count"]) and np.array_equal(after["pos"], want["pos"])
     assert np.array_equal(after["k"], want["k"], equal_nan=True) and np.array_equal(after["v"], want["v"], equal_nan=True)
     near("score", after["score"], want["score"], bound["score"])
-    near("lse", lse.double().cpu().numpy().reshape(l64.shape), l64, bound["lse"])
-    near("o", o.double().cpu().numpy().reshape(o64.shape), o64, bound["o"])
+    near("lse", of(lse, 1).double().cpu().numpy().reshape(l64.shape), l64, bound["lse"])
+    near("o", of(o, s.d).double().cpu().numpy().reshape(o64.shape), o64, bound["o"])
     return o, lse
 
 

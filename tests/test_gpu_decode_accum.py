@@ -76,10 +76,10 @@ class Run:
             return lte.lte_attn_decode4_accum(self.s, self.cache, q, k, v, decay=decay, **kw)
         return lte.lte_attn_decode4(self.s, self.conv, self.cache, q, k, v, **kw)
 
-    def step(self, decay=1.0, tokens=None):
+    def step(self, decay=1.0, tokens=None, which=None):
         q, k, v = tokens or self.tokens()
         f = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
-        return ref.check_step(self.s, self.lay, self.cache, q, k, v, lambda: self.call(q, k, v, decay), self.kind != "four learned", decay, f(self.w), f(self.bias))
+        return ref.check_step(self.s, self.lay, self.cache, q, k, v, lambda: self.call(q, k, v, decay), self.kind != "four learned", decay, f(self.w), f(self.bias), which)
 
 
 KINDS = ["accum", "four accum", "four learned"]
@@ -108,6 +108,24 @@ def test_steps(kind, dtype, B, H, G, d, W, R, n, cnt, sink, K):
     for i in range(6):
         r.step(decay=(1.0, 0.9, 0.0)[i % 3])
     assert lte.lte_device_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["accum", "four accum"])
+@pytest.mark.parametrize("B,H,G,d,W,R,n,cnt", [
+    (80, 16, 17, 32, 150, 150, 900, 150),              # a warp a head, three passes of query heads
+    (100, 16, 9, 64, 100, 156, 700, 156),              # the same, swizzled rows
+    (100, 16, 8, 64, 120, 137, 1000, 90),              # the pool not full
+    (32, 16, 12, 64, 900, 1100, 890, 0),               # several warps a head, the ring not full
+    (32, 16, 12, 64, 600, 1400, 5000, 1400),
+    (20, 15, 17, 128, 500, 1000, 9000, 1000),
+    (2, 37, 9, 32, 1000, 5000, 30000, 5000),           # a cluster a head
+])
+def test_scores_of_heads_whose_logits_do_not_fit(kind, B, H, G, d, W, R, n, cnt):
+    """So many rows, query heads and heads at once that the logits of an SM's heads do not fit its shared memory: the weights come from the
+    keys, read once more."""
+    r = Run(kind, "bf16", B, H, G, d, W, R, n, cnt, sink=1)
+    for decay in (0.9, 0.0):
+        r.step(decay=decay, which=[0, 1, H - 1, B * H // 2, B * H - 1])
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
