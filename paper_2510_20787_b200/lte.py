@@ -203,9 +203,9 @@ def lte_attn_decode(s, c, cache, q1, k1, v1, o1=None, lse1=None):
     return (_native or _load()).attn_decode(s, c, cache, q1, k1, v1, o1, lse1)
 
 
-def _new_cache(n, s, like):
-    if n == 0:
-        raise LteError("lte_cache_bytes", -2)
+def _new_cache(fn, n, like):
+    if n == 0:                                                 # a shape that no call takes
+        raise LteError(fn, -2)
     return torch.empty(n, dtype=torch.uint8, device=like.device if like is not None else torch.device("cuda"))
 
 
@@ -213,7 +213,7 @@ def lte_cache_init_accum(s, k=None, v=None, a=None, idx=None, cnt=None, cache=No
     """Decode cache whose rows are ranked by accumulated attention: a [B,H,T] fp32 of lte_attn_colsum, the list of
     lte_select_rule(RULE_ACCUM_ATTN) (T = 0: empty cache)."""
     if cache is None:
-        cache = _new_cache(lte_cache_bytes(s), s, k)
+        cache = _new_cache("lte_cache_init_accum", lte_cache_bytes(s), k)
     return (_native or _load()).cache_init_accum(s, k, v, a, idx, cnt, cache)
 
 
@@ -231,14 +231,14 @@ def lte_cache4_bytes(s):
 def lte_cache4_pack(s, cache, cache4=None):
     """An ordinary cache (lte_cache_init, lte_cache_init_accum) rounded to 4 bits."""
     if cache4 is None:
-        cache4 = _new_cache(lte_cache4_bytes(s), s, cache)
+        cache4 = _new_cache("lte_cache4_pack", lte_cache4_bytes(s), cache)
     return (_native or _load()).cache4_convert(s, cache, cache4, True)
 
 
 def lte_cache4_unpack(s, cache4, cache=None):
     """A cache in 4 bits as an ordinary one of s.dtype, e.g. for lte_attn_prefill_chunk."""
     if cache is None:
-        cache = _new_cache(lte_cache_bytes(s), s, cache4)
+        cache = _new_cache("lte_cache4_unpack", lte_cache_bytes(s), cache4)
     return (_native or _load()).cache4_convert(s, cache4, cache, False)
 
 
