@@ -468,6 +468,7 @@ static int decode_rows(const lte_shape* s, const lte_conv* c, bool four, bool ac
         if (!(decay >= 0.f && decay <= 1.f)) return LTE_ERR_INVALID_ARG;
     } else {
         e = check_conv(s, c); if (e) return e;
+        if (!aligned(c->w, 4) || !aligned(c->bias, 4)) return LTE_ERR_INVALID_ARG;
     }
     if (!cache || !q1 || !k1 || !v1 || !o1 || !lse1) return LTE_ERR_INVALID_ARG;
     if (!aligned16(cache) || !aligned16(q1) || !aligned16(k1) || !aligned16(v1) || !aligned(o1, element_bytes(s)) || !aligned(lse1, 4)) return LTE_ERR_INVALID_ARG;

@@ -41,7 +41,8 @@ def test_refusals():
         for decay in (-0.01, 1.01, float("nan"), float("inf")):
             assert call(kind, 1, decay) == -1
     assert call("four", 1, None) == -1
-    for bad, status in ((lte.LteConv(1, 6, 1, 256, 0), -1), (lte.LteConv(1, 17, 1, 256, 0), -1), (lte.LteConv(1, 7, 1, 0, 0), -1), (lte.LteConv(3, 3, 2, 256, 0), -2)):
+    for bad, status in ((lte.LteConv(1, 6, 1, 256, 0), -1), (lte.LteConv(1, 17, 1, 256, 0), -1), (lte.LteConv(1, 7, 1, 0, 0), -1), (lte.LteConv(1, 7, 1, 258, 0), -1), (lte.LteConv(1, 7, 1, 256, 258), -1),
+                        (lte.LteConv(3, 3, 2, 256, 0), -2)):
         assert call("four", 1, a(bad)) == status
     narrow = lte.shape(1, 2, 0, 64, 5, 8, lte.BF16)
     assert call("four", 0, a(narrow)) == -1                    # a window shorter than the receptive field

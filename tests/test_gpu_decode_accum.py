@@ -272,6 +272,17 @@ def test_two_streams_at_once(kind, dtype):
         assert torch.equal(r.cache, w.cache)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 32)])
+def test_scorer_weights_off_a_16_byte_boundary(dtype, d):
+    a, b = (Run("four learned", dtype, 2, 3, 2, d, 40, 30, 300, 30, K=9) for _ in range(2))
+    b.conv = lte.conv(torch.cat([b.w.new_zeros(1), b.w.flatten()])[1:].view(b.w.shape), b.bias)
+    for _ in range(3):
+        t = a.tokens()
+        for x, y in zip(a.call(*t), b.call(*t)):
+            assert torch.equal(x, y)
+    assert torch.equal(a.cache, b.cache)
+
+
 def test_caches_past_4_gigabytes():
     """The last heads of a cache whose offsets pass 32 bits."""
     B, H, d, W, R = 9, 32, 128, 2768, 30000
