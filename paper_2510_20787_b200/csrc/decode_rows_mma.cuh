@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     auto s_acc = [&](int w, int u) { return reinterpret_cast<float*>(s_dyn + w * (STAGES * St::BYTES)) + u * PITCH; };
     __shared__ float s_unit[MQ];
     __shared__ float s_m[NW][MQ], s_l[NW][MQ], s_new[MQ];
-    __shared__ float s_in[2][SPLIT > 1 ? MQ * D : 1];
+    __shared__ float s_in[2][SPLIT > 1 ? MQ * D + SPLIT : 1];
     __shared__ __align__(16) float s_ml[2][SPLIT][MQ][2];      // the cluster's shares of this block's output elements (by pass parity)
     __shared__ __align__(16) __nv_bfloat16 s_kv[2][D];         // the incoming token
     __shared__ float s_tap[NW];
@@ -747,7 +747,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         }
         __syncthreads();
         if (shared_head && g0 == 0 && !met) cluster.barrier_wait();    // every block of the cluster has started: its shared memory is there
-        const int per = nq * D / nsplit, par = (g0 / MQ) & 1;  // output elements each block of the cluster finishes
+        const int per = (nq * D + nsplit - 1) / nsplit, par = (g0 / MQ) & 1;  // output elements each block of the cluster finishes
         // Lane u of every warp: reference and sum of query u over this block's rows (and the incoming token, in the first block)
         float qm = -FLT_MAX, qt = 0.f, qs = 0.f;
         if (lane < nq) {
@@ -785,11 +785,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             qi = 1.f / qt;
             if (rank == 0 && wid == 0 && lane < nq) lse1[(size_t)bh * G + g0 + lane] = qm * (scale * s_unit[lane]) + logf(qt);
             for (int e0 = wid * 32; e0 < per; e0 += NT) {
-                const int e = min(e0 + lane, per - 1), el = rank * per + e, u = el / D, ch = el - u * D;
+                const int e = min(e0 + lane, per - 1), el = min(rank * per + e, nq * D - 1), u = el / D, ch = el - u * D;
                 const float m = __shfl_sync(0xffffffffu, qm, u), inv = __shfl_sync(0xffffffffu, qi, u), sq = __shfl_sync(0xffffffffu, qs, u);
                 float o = 0.f;
                 for (int r2 = 0; r2 < nsplit; ++r2) o = fmaf(exp2_fast((s_ml[par][r2][u][0] - m) * sq), s_in[par][r2 * per + e], o);
-                if (e0 + lane < per) o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * inv);
+                if (e0 + lane < per && rank * per + e < nq * D) o1[((size_t)bh * G + g0 + u) * D + ch] = __float2bfloat16_rn(o * inv);
             }
         }
         if constexpr (RULE == KEPT) {
@@ -911,6 +911,35 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     }
 }
 
+constexpr size_t kMostSmem = 200 * 1024;                       // dynamic, of a block
+
+// The most blocks that a cluster of a head may have so that `heads` of them run at once with one block to an SM; 0 where not even single blocks do.
+// (Clusters lie within a group of SMs, and the groups differ in size: of 148 SMs, 7 clusters of 16 find room, 11 of 10, 15 of 8 or 9, 22 of 6, 33 of 4.)
+template <bool FOUR, bool ACCUM>
+int one_block_an_sm(int heads, int* blocks)
+{
+    struct Counts { int of[MAX_SPLIT + 1]; };                  // clusters at a time, by their blocks
+    static PerDevice<Counts> table;
+    Counts n;
+    if (int e = table.get(&n, [&](Counts* out) {
+            auto kern = decode_rows_mma_kernel<128, MAX_WARPS, FOUR ? 3 : 2, false, FOUR, ACCUM ? KEPT : LEARNED>;
+            if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) return cuda_status(x);
+            if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) return cuda_status(x);
+            for (int c = 1; c <= MAX_SPLIT; ++c) {
+                cudaLaunchConfig_t cfg = {};
+                cudaLaunchAttribute attr;
+                attr.id = cudaLaunchAttributeClusterDimension;
+                attr.val.clusterDim.x = c; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+                cfg.gridDim = dim3(c); cfg.blockDim = dim3(MAX_WARPS * 32); cfg.dynamicSmemBytes = kMostSmem;
+                cfg.attrs = &attr; cfg.numAttrs = 1;
+                if (cudaOccupancyMaxActiveClusters(&out->of[c], kern, &cfg) != cudaSuccess) { (void)cudaGetLastError(); out->of[c] = 0; }
+            }
+            return (int)LTE_OK; })) return e;
+    *blocks = n.of[MAX_SPLIT] > 0 ? MAX_SPLIT : 8;             // (a launch takes more than 8 only where 16 are possible)
+    while (*blocks > 0 && n.of[*blocks] < heads) --*blocks;
+    return LTE_OK;
+}
+
 // How many warps share a head: all warps of the launch are resident at once where that is possible, as in decode_mma.cu.
 template <bool FOUR, bool ACCUM>
 int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1,
@@ -921,8 +950,8 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm;
     const int UR = FOUR || p.d < 128 ? 32 : 16;                // rows that a warp takes at a time (Stage::UR)
     // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, take 39.5 us with four warps,
-    // 30.9 with eight (bf16; 4-bit blocks of eight take an SM's registers: 24.1 and 33.0).  16 heads x 1,024 rows take 7.9 us with four warps in
-    // clusters of 8 and 13.1 with eight (4 bits, d = 128).  Clusters of 16 only where each block has an SM to itself: 16 heads took as long as 32.
+    // 30.9 with eight (bf16; a 4-bit block of eight takes an SM's registers, and clusters of those are for `wide` below).  Clusters of 16 only where
+    // each block may have an SM to itself: 16 heads took as long as 32.
     const bool is_long = rows > 4096;
     const int most_w = p.d == 128 && (FOUR || !is_long) ? 4 : MAX_WARPS, most_split = is_long ? MAX_SPLIT : 8;
     int nw = 1, nsplit = 1;
@@ -945,6 +974,24 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         const size_t block = smem(most_w, more) + (size_t)most_w * 8 * 1024 + 12 * 1024;   // with its stages (8 KB a warp)
         if (block * (wps / most_w) <= 224 * 1024 && (long long)BH * more <= 2ll * n_sm * (wps / most_w)) { keep = true; nw = most_w; nsplit = more; }
     }
+    // Heads that leave an SM one block take blocks of eight warps with a stage more, in clusters of which every block finds an SM of its own: two
+    // on one SM take as long as one with the rows of both, and a block of eight 4-bit warps that finds none waits for the whole step of another.
+    // us a step without | with (four query heads; bf16 accumulated, 4 bits learned):
+    //   d = 128    8 heads x 17,408 rows   29.3 | 27.4, 18.5 | 16.6       12 x 17,408   46.6 | 29.9, 28.1 | 18.9       16 x 17,408   47.9 | 39.9, 28.4 | 23.8
+    //              8 x 4,024   16.5 | 13.3, 11.4 | 10.0       32 x 2,560   22.0 | 16.2, 14.2 | 10.8       32 x 384   12.7 | 8.9, 12.0 | 8.4
+    //              148 x 1,248   36.0 | 22.2, 14.8 | 12.6       128 x 1,536   25.5 | 23.5, 16.1 | 14.3       64 x 1,536   20.0 | 17.6, 11.8 | 11.5
+    //   d = 64     16 x 17,408   31.1 | 26.8, 19.4 | 23.3       32 x 384   8.2 | 7.9       32 x 1,024   11.3 | 8.4       128 x 1,536   17.0 | 16.1
+    // so not 4 bits at d = 64 (32 codes a lane leave 16 warps room).  Not few rows either (8 x 1,024, bf16: 9.9 | 9.1 at d = 128, 7.9 | 8.1 at d = 64;
+    // 4 bits accumulated 9.6 | 9.8; 128 x 96, d = 64: 5.8 | 6.1).  Long bf16 rows need many SMs: 64 x 6,024 take 32.8 | 34.4 at d = 128, 20.9 | 22.5
+    // at d = 64, 28 x 17,408 (112 SMs) 50.6 | 54.9, but 40 x 6,024 (120) 29.5 | 25.3.
+    bool wide = false;
+    if ((FOUR ? p.d == 128 : p.d >= 64) && rows >= 128 && BH <= n_sm && (long long)BH * rows >= 12288) {
+        int c = 0;
+        if (int e = one_block_an_sm<FOUR, ACCUM>(BH, &c)) return e;
+        const bool fits = !ACCUM || (c > 0 && smem(MAX_WARPS, c) + MAX_WARPS * (FOUR ? 3 * 5 : 2 * 8) * 1024 <= kMostSmem);
+        const bool enough = rows <= 2048 || c >= 6 || (c != 2 && BH * c * 5 >= n_sm * 4);
+        if (c > 0 && (FOUR || (fits && enough))) { wide = true; keep = fits; nw = MAX_WARPS; nsplit = c; }
+    }
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
         auto with_kind = [&](auto stages, auto kind) {
@@ -956,7 +1003,6 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
             attr[0].val.programmaticStreamSerializationAllowed = 1;
             attr[1].id = cudaLaunchAttributeClusterDimension;
             attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-            constexpr size_t kMostSmem = 200 * 1024;
             static PerDevice<int> table;                       // blocks that a cluster may have, and the kernel's limits raised
             int split_most = 1;
             if (int e = table.get(&split_most, [&](int* out) {
@@ -988,6 +1034,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
         };
         // two stages a warp; three where eight warps of an SM have the room, one where 16 have not (bf16 at d = 128: 8 KB a stage), unless few
         // heads leave it (16 x 1,024 rows: 9.7 us with one, 9.3 with two)
+        if constexpr (!FOUR && D >= 64 && NW == MAX_WARPS && !decltype(s)::value) { if (wide) return with(std::integral_constant<int, 2>()); }
         if constexpr (D < 128) return with(std::integral_constant<int, FOUR || D == 32 ? 2 : 1>());
         else if constexpr (FOUR) return with(std::integral_constant<int, 3>());
         else if constexpr (NW == 4) return BH * nsplit * NW <= 8 * n_sm ? with(std::integral_constant<int, 2>()) : with(std::integral_constant<int, 1>());

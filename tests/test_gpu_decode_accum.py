@@ -110,6 +110,36 @@ def test_steps(kind, dtype, B, H, G, d, W, R, n, cnt, sink, K):
     assert lte.lte_device_status() == 0
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,H,G,d,W,R,n,cnt", [
+    (1, 8, 3, 128, 700, 1300, 4000, 1300),             # (on 148 SMs: clusters of 10; their shares of the outputs are of unequal sizes
+    (1, 12, 1, 64, 512, 700, 3000, 690),               # of 9
+    (2, 8, 5, 128, 300, 600, 900, 600),                # of 6
+    (2, 13, 7, 128, 100, 500, 700, 500),               # of 5
+    (4, 9, 9, 128, 130, 300, 700, 300),                # of 3, two passes of query heads
+    (4, 10, 3, 64, 100, 250, 99, 0),                   # of 3, the ring not full
+    (11, 6, 17, 64, 128, 128, 500, 128),               # of 2, swizzled rows, three passes of query heads
+    (37, 4, 2, 128, 100, 29, 1000, 29),                # one block a head
+    (37, 4, 1, 64, 100, 70, 3, 0),                     # the same, hardly a row
+    (1, 4, 8, 128, 2048, 4000, 30000, 4000),           # of 16
+])
+def test_blocks_of_eight_warps_one_an_sm(kind, B, H, G, d, W, R, n, cnt):
+    r = Run(kind, "bf16", B, H, G, d, W, R, n, cnt, sink=1)
+    for decay in (0.9, 1.0, 0.0):
+        r.step(decay=decay, which=[0, 1, H - 1, B * H // 2, B * H - 1])
+    assert lte.lte_device_status() == 0
+
+
+@pytest.mark.parametrize("B,H,G,d,W,R,n,cnt", [
+    (1, 8, 8, 128, 1000, 28000, 90000, 28000),         # logits do not fit beside the stages of eight warps: the keys once more
+    (1, 5, 11, 128, 2000, 30768, 90000, 30768),
+])
+def test_scores_of_long_4_bit_rows(B, H, G, d, W, R, n, cnt):
+    r = Run("four accum", "bf16", B, H, G, d, W, R, n, cnt, sink=1)
+    for decay in (0.9, 0.0):
+        r.step(decay=decay, which=[0, H - 1])
+
+
 @pytest.mark.parametrize("kind", ["accum", "four accum"])
 @pytest.mark.parametrize("B,H,G,d,W,R,n,cnt", [
     (80, 16, 17, 32, 150, 150, 900, 150),              # a warp a head, three passes of query heads
