@@ -29,8 +29,8 @@
 //   256 x 1,280, four query heads each, d = 64           20.3 (13.3)          14.7 (4.5)            12.8 (4.2)
 //   2,048 x 1,024, d = 64                                 108 (85.3)          58.8 (28.8)           51.9 (26.9)
 //   512 x 1,024, d = 128                                 47.4 (41.9)          28.8 (13.6)
-//   8 x 17,408, four query heads each, d = 128           29.3 (11.1)          23.0 (3.7)            18.4 (3.6)
-//   16 x 1,024, d = 128 (one user)                        9.0 (1.3)            8.4 (0.4)             7.9 (0.4)
+//   8 x 17,408, four query heads each, d = 128           27.3 (11.1)          19.8 (3.7)            16.5 (3.6)
+//   16 x 1,024, d = 128 (one user)                        8.6 (1.3)            8.7 (0.4)             7.7 (0.4)
 // Of a step 5 to 8 us are the chain of launch, counters, first rows, meeting and write-back (what 32 rows a head take).  What did not help: 4-bit
 // rows in 80 registers and 24 warps an SM (2,048 x 256: 27.8), bulk copies with a barrier per stage in the place of 16-byte ones (the same for bf16,
 // and 35 instructions per 16 rows more), codes as bf16 numbers 16 + c with P in two terms (1.05 us per 16 rows of 2,048 heads, now 0.67).
