@@ -18,8 +18,10 @@
 //            row, are applied to the products in fp32 (a lane holds rows of both).  q is scaled by a power of two per query head to at most 2^15 (and
 //            by 1/16 where it meets 16 c), in which fp16 holds bf16 numbers exactly down to 2^-24; logits are kept in that scale;
 //   output   P step takes the place of P, per group, and P zero, the same for all channels of a group, is summed beside it in fp32.  P step is
-//            rounded to fp16, 2^-12 of it: an error of o of at most 2^-12 sum(w c step), a tenth of the rounding of o itself in the mean square (o
-//            against 64 bits: 1.7e-3 before and after).  It is scaled by a power of two, the same for the warp, that follows the largest step.
+//            rounded to fp16, 2^-12 of it: an error of o of at most 2^-12 sum(w c step) (o against 64 bits, in the mean square: 1.67e-3 to 1.73e-3,
+//            1.66e-3 with the rounding of o alone).  It is scaled by a power of two, per group and query, that follows the largest product
+//            (not the largest step: a row whose weight is nothing may have any).  That stands at 2^11 or above, so that one too
+//            small for fp16's normal numbers is off by 2^-36 of it.
 // The contraction index may be permuted freely: the nibbles i and i + 4 of a key word are neighbours in it, and so are the two rows whose value
 // units a byte permute joins.  The order of the codes in the cache (cache4.cuh) makes these the words that a lane loads.
 //
@@ -92,9 +94,8 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
     struct Query { uint4 f[KP]; float unit[2]; };
     struct Acc { float a[MT][4]; };
     struct Pars {};
-    static __device__ __forceinline__ float load_pars(Pars&, uint32_t, int, int) { return 0.f; }
-    static __device__ __forceinline__ bool too_large(const Acc&, float) { return false; }
-    static __device__ __forceinline__ void lower(Acc&, float) {}
+    struct Weights {};
+    static __device__ __forceinline__ void load_pars(Pars&, uint32_t, int, int) {}
     static __device__ __forceinline__ int rho(int g) { return g; }
     static __device__ __forceinline__ void load_q(Raw& r, const __nv_bfloat16* q, bool some, int g, int t)
     {
@@ -153,7 +154,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
             if (lane < D / 8) *reinterpret_cast<uint4*>(st + Stage<D, false>::V + (__ffs(gone) - 1) * PITCH + 16 * lane) = make_uint4(0, 0, 0, 0);
     }
     // Lane (g, t) takes pieces g, g + 8 of rows 2t, 2t + 1, 2t + 8, 2t + 9.
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars&, uint32_t st, int span, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Weights&, const Pars&, uint32_t st, int span, int g, int t)
     {
         uint32_t v[4][VB];
 #pragma unroll
@@ -192,10 +193,12 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 // rho(2t + b + 8c) = t + 4b + 8c: the value units that the lanes load at once then lie in different banks.
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static constexpr int GR = D / kGroup4, MT = D / 16;
+    static constexpr uint32_t MOST_INV = 246u;                 // exponent of the largest scale, 2^119 (times a weight, below 2^8: finite)
     static constexpr float LIFT = 16777216.f;                  // 2^24: logits are kept as sums of c 2^-24 q
     struct Raw { uint4 u[GR]; };                               // channels 8t .. 8t + 7 of every group of query g
     struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and inverse scales of queries 2t, 2t + 1
-    struct Acc { float a[MT][4], z[GR][2], inv; };             // inv: the scale of P step
+    struct Acc { float a[MT][4], z[GR][2], inv[GR][2]; };      // inv: the scale of P step, per group and query
+    struct Weights { uint32_t h[GR][2]; };                     // P step inv of two queries, of rows rho(g), rho(g) + 8
     struct Pars { uint32_t p[2][GR]; };                        // of rows rho(g), rho(g) + 8
     static __device__ __forceinline__ int rho(int g) { return (g >> 1) + 4 * (g & 1); }     // (g < 8)
     static __device__ __forceinline__ void load_q(Raw& r, const __nv_bfloat16* q, bool some, int g, int t)
@@ -272,14 +275,36 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         for (int m = 0; m < MT; ++m) A.a[m][0] = A.a[m][1] = A.a[m][2] = A.a[m][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < GR; ++j) A.z[j][0] = A.z[j][1] = 0.f;
-        A.inv = 0x1p127f;
+#pragma unroll
+        for (int j = 0; j < GR; ++j) A.inv[j][0] = A.inv[j][1] = __uint_as_float(MOST_INV << 23);
     }
-    static __device__ __forceinline__ void rescale(Acc& A, float f0, float f1)
+    // A new reference, under which weights are f0, f1 times as large (at most 1) and this unit's are p.  A scale takes f up, rounded up to a power of
+    // two, as far as it can, so that the largest product so far does not get smaller in fp16; where the unit has a product above 2^15, its scale goes
+    // to where the largest is 2^11 .. 2^12, which leaves four binary places for later ones.
+    template <int UNIT> static __device__ __forceinline__ void rescale(Acc& A, float f0, float f1, const float (&p)[UNIT][4], const Pars (&P)[UNIT])
     {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) { A.a[m][0] *= f0; A.a[m][1] *= f1; A.a[m][2] *= f0; A.a[m][3] *= f1; }
+        for (int e = 0; e < 2; ++e) {
+            const float f = e ? f1 : f0;
+            const uint32_t up = 127u - min(__float_as_uint(f) >> 23, 127u);
 #pragma unroll
-        for (int j = 0; j < GR; ++j) { A.z[j][0] *= f0; A.z[j][1] *= f1; }
+            for (int j = 0; j < GR; ++j) {
+                float top = 0.f;                               // 2^-10 of the largest (which need not be finite)
+#pragma unroll
+                for (int x = 0; x < UNIT; ++x)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) top = fmaxf(top, p[x][2 * u + e] * 0x1p-10f * par4_step(P[x].p[u][j]));
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const uint32_t old = __float_as_uint(A.inv[j][e]) >> 23, raised = min(old + up, MOST_INV);
+                const uint32_t now = top * __uint_as_float(raised << 23) > 32.f ? min(255u - (__float_as_uint(top) >> 23), MOST_INV) : raised;
+                const float part = f * __uint_as_float((127u + raised - old) << 23) * __uint_as_float((uint32_t)max(127 + (int)now - (int)raised, 0) << 23);
+                A.inv[j][e] = __uint_as_float(now << 23);
+                A.z[j][e] *= f;
+#pragma unroll
+                for (int m = 2 * j; m < 2 * j + 2; ++m) { A.a[m][e] *= part; A.a[m][2 + e] *= part; }
+            }
+        }
     }
     // what the rows of a unit that `gone` names hold as values: with step and zero 0 it is 0
     static __device__ __forceinline__ void clear(unsigned char* st, unsigned gone, int lane)
@@ -289,30 +314,29 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             for (int j = 0; j < GR; ++j) reinterpret_cast<uint32_t*>(st + Stage<D, true>::VP)[lane * GR + j] = 0u;
     }
     // parameters of a span's values
-    static __device__ __forceinline__ float load_pars(Pars& P, uint32_t st, int span, int g)
+    static __device__ __forceinline__ void load_pars(Pars& P, uint32_t st, int span, int g)
     {
-        float top = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            lds(P.p[u], st + rho(g) * (4 * GR) + Stage<D, true>::VP + (2 * span + u) * (32 * GR));
+        for (int u = 0; u < 2; ++u) lds(P.p[u], st + rho(g) * (4 * GR) + Stage<D, true>::VP + (2 * span + u) * (32 * GR));
+    }
+    // A span's weights times the steps of its rows, as the second product's operand.  True where one of this lane's is above 2^15.
+    // (The scale meets the weight first: a row that weighs next to nothing may have any step.)
+    static __device__ __forceinline__ bool weigh(Weights& w, const Acc& A, const float (&p)[4], const Pars& P)
+    {
+        __half2 top = __floats2half2_rn(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < GR; ++j) top = fmaxf(top, par4_step(P.p[u][j]));
+        for (int j = 0; j < GR; ++j) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float s = par4_step(P.p[u][j]);
+                const __half2 x = __floats2half2_rn(p[2 * u] * A.inv[j][0] * s, p[2 * u + 1] * A.inv[j][1] * s);
+                top = __hmax2(top, x);
+                w.h[j][u] = *reinterpret_cast<const uint32_t*>(&x);
+            }
         }
-        return top;
+        return __hgt2_mask(top, __floats2half2_rn(32768.f, 32768.f)) != 0u;
     }
-    // P step stays below 2^15: weights below 2^8, step inv below 2^7.  Where a lane's largest step passes that, inv goes to where the largest of
-    // the warp has four binary places left.
-    static __device__ __forceinline__ bool too_large(const Acc& A, float top) { return top * A.inv > 128.f; }
-    static __device__ __forceinline__ void lower(Acc& A, float top)
-    {
-        top = warp_max(top);
-        if (!too_large(A, top)) return;
-        const float inv = __uint_as_float(min(257u - (__float_as_uint(top) >> 23), 254u) << 23), f = inv / A.inv;
-        A.inv = inv;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) { A.a[m][0] *= f; A.a[m][1] *= f; A.a[m][2] *= f; A.a[m][3] *= f; }
-    }
-    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Pars& P, uint32_t st, int span, int g, int t)
+    static __device__ __forceinline__ void output(Acc& A, const float (&p)[4], const Weights& W, const Pars& P, uint32_t st, int span, int g, int t)
     {
         const uint32_t values = st + t * (D / 2) + g * (2 * GR) + Stage<D, true>::V + span * (8 * D);
         uint32_t v[4][(GR + 1) / 2];
@@ -331,9 +355,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             const float z0 = par4_zero(P.p[0][j]), z1 = par4_zero(P.p[1][j]);
             A.z[j][0] = fmaf(p[2], z1, fmaf(p[0], z0, A.z[j][0]));
             A.z[j][1] = fmaf(p[3], z1, fmaf(p[1], z0, A.z[j][1]));
-            const float s0 = par4_step(P.p[0][j]) * A.inv, s1 = par4_step(P.p[1][j]) * A.inv;
-            const __half2 x0 = __floats2half2_rn(p[0] * s0, p[1] * s0), x1 = __floats2half2_rn(p[2] * s1, p[3] * s1);
-            const uint32_t h0 = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&x0)), h1 = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&x1));
+            const uint32_t h0 = movmatrix_trans(W.h[j][0]), h1 = movmatrix_trans(W.h[j][1]);
             const uint32_t u = __byte_perm(v[0][j / 2], v[1][j / 2], j & 1 ? 0x7632 : 0x5410), u8 = u >> 8;   // four codes of M-row 2t, of M-row 2t + 1
             const uint32_t w = __byte_perm(v[2][j / 2], v[3][j / 2], j & 1 ? 0x7632 : 0x5410), w8 = w >> 8;
             mma16816_f16(A.a[2 * j], u & 0x000f000fu, u & 0x00f000f0u, w & 0x000f000fu, w & 0x00f000f0u, h0, h1);
@@ -350,7 +372,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
                 float z = A.z[j][e];
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-                const float back = 1.f / A.inv;                // (the second channel of a pair: sums of 16 c)
+                const float back = __uint_as_float((254u << 23) - __float_as_uint(A.inv[j][e]));   // (the second channel of a pair: sums of 16 c)
 #pragma unroll
                 for (int m = 2 * j; m < 2 * j + 2; ++m) {
                     A.a[m][e] = fmaf(A.a[m][e] * LIFT, back, z);
@@ -678,16 +700,40 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 kept += UR;
             }
             typename Gr::Pars vpar[UNIT];
-            float steps = 0.f;
+            typename Gr::Weights weights[UNIT];
 #pragma unroll
-            for (int x = 0; x < UNIT; ++x) steps = fmaxf(steps, Gr::load_pars(vpar[x], st, x, g));
+            for (int x = 0; x < UNIT; ++x) Gr::load_pars(vpar[x], st, x, g);
             // The reference m follows the maximum only when that has grown by 2^8 (weights stay below 2^8, in fp32): a vote per
-            // unit instead of a reduction over its rows.
-            float x0 = fmaxf(c[0][0], c[0][2]), x1 = fmaxf(c[0][1], c[0][3]);
+            // unit instead of a reduction over its rows.  4 bits: the same vote says whether a product with a step has grown too large.
+            auto exponentials = [&]() {                        // p from c
 #pragma unroll
-            for (int x = 1; x < UNIT; ++x) { x0 = fmaxf(x0, fmaxf(c[x][0], c[x][2])); x1 = fmaxf(x1, fmaxf(c[x][1], c[x][3])); }
-            if (__any_sync(0xffffffffu, fmaf(x0, Gr::LIFT, -m0) > jump0 || fmaf(x1, Gr::LIFT, -m1) > jump1 || Gr::too_large(acc, steps))) {
-                float y0 = x0 * Gr::LIFT, y1 = x1 * Gr::LIFT;
+                for (int x = 0; x < UNIT; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast(fmaf(c[x][e], Gr::LIFT, e & 1 ? -m1 : -m0) * (e & 1 ? sq1 : sq0));
+            };
+            auto times_steps = [&]() {                         // 4 bits: true where a product is too large
+                bool over = false;
+                if constexpr (FOUR)
+#pragma unroll
+                    for (int x = 0; x < UNIT; ++x) over |= Gr::weigh(weights[x], acc, p[x], vpar[x]);
+                return over;
+            };
+            auto largest = [&](const float (&y)[UNIT][4], int e) {
+                float x = fmaxf(y[0][e], y[0][2 + e]);
+#pragma unroll
+                for (int u = 1; u < UNIT; ++u) x = fmaxf(x, fmaxf(y[u][e], y[u][2 + e]));
+                return x;
+            };
+            bool far;
+            if constexpr (FOUR) {
+                exponentials();
+                far = fmaxf(largest(p, 0), largest(p, 1)) > 256.f;
+                far |= times_steps();
+            } else {
+                far = fmaf(largest(c, 0), Gr::LIFT, -m0) > jump0 || fmaf(largest(c, 1), Gr::LIFT, -m1) > jump1;
+            }
+            if (__any_sync(0xffffffffu, far)) {
+                float y0 = largest(c, 0) * Gr::LIFT, y1 = largest(c, 1) * Gr::LIFT;
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) {
                     y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, o));
@@ -697,17 +743,19 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 const float f0 = exp2_fast((m0 - y0) * sq0), f1 = exp2_fast((m1 - y1) * sq1);
                 m0 = y0; m1 = y1;
                 l0 *= f0; l1 *= f1;
-                Gr::rescale(acc, f0, f1);
-                Gr::lower(acc, steps);
+                if constexpr (FOUR) {
+                    exponentials();
+                    Gr::rescale(acc, f0, f1, p, vpar);
+                    (void)times_steps();
+                } else {
+                    Gr::rescale(acc, f0, f1);
+                }
             }
+            if (!FOUR) exponentials();
 #pragma unroll
-            for (int x = 0; x < UNIT; ++x) {
+            for (int x = 0; x < UNIT; ++x) { l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3]; }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[x][e] = exp2_fast(fmaf(c[x][e], Gr::LIFT, e & 1 ? -m1 : -m0) * (e & 1 ? sq1 : sq0));
-                l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3];
-            }
-#pragma unroll
-            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], vpar[x], st, x, g, t);
+            for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], weights[x], vpar[x], st, x, g, t);
             __syncwarp();                                      // every lane has read the stage
             if (FOUR) ask_keys(st);
             ask_values(st);
