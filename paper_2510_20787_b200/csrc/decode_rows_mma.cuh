@@ -194,9 +194,12 @@ template <int D, bool SWZ> struct Group<D, SWZ, false> {
 template <int D, bool SWZ> struct Group<D, SWZ, true> {
     static constexpr int GR = D / kGroup4, MT = D / 16;
     static constexpr uint32_t MOST_INV = 246u;                 // exponent of the largest scale, 2^119 (times a weight, below 2^8: finite)
-    static constexpr float LIFT = 16777216.f;                  // 2^24: logits are kept as sums of c 2^-24 q
+    static constexpr float CODE = 16777216.f;                  // 2^24: products are sums of c 2^-24 q
+    // A logit is the product, times LIFT, times the query's unit, which has the rest of CODE: split so that neither the products of keys as large as
+    // 2^120 nor the units of the largest queries leave the range of fp32.
+    static constexpr float LIFT = 1024.f, UNIT = CODE / LIFT;
     struct Raw { uint4 u[GR]; };                               // channels 8t .. 8t + 7 of every group of query g
-    struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and inverse scales of queries 2t, 2t + 1
+    struct Query { uint32_t f[GR][4]; float sum[GR][2], unit[2]; };   // of query g, scaled; sums over a group's channels and units of queries 2t, 2t + 1
     struct Acc { float a[MT][4], z[GR][2], inv[GR][2]; };      // inv: the scale of P step, per group and query
     struct Weights { uint32_t h[GR][2]; };                     // P step inv of two queries, of rows rho(g), rho(g) + 8
     struct Pars { uint32_t p[2][GR]; };                        // of rows rho(g), rho(g) + 8
@@ -219,7 +222,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // the power of two that takes the largest channel to 2^14 .. 2^15 (1 for a query that is zero or not finite)
         const uint32_t ex = __float_as_uint(top) >> 23, field = top > 0.f && top < INFINITY ? min(268u - ex, 253u) : 127u;
-        const float scale = __uint_as_float(field << 23), unit = __uint_as_float((254u - field) << 23);
+        const float scale = __uint_as_float(field << 23), unit = __uint_as_float((254u - field) << 23) * UNIT;
 #pragma unroll
         for (int j = 0; j < GR; ++j) {
             float x[8], s = 0.f;
@@ -236,7 +239,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
             }
             s += __shfl_xor_sync(0xffffffffu, s, 1);
             s += __shfl_xor_sync(0xffffffffu, s, 2);
-            s *= 1.f / LIFT;
+            s *= 1.f / CODE;
             Q.sum[j][0] = __shfl_sync(0xffffffffu, s, 8 * t);
             Q.sum[j][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
         }
@@ -375,8 +378,8 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
                 const float back = __uint_as_float((254u << 23) - __float_as_uint(A.inv[j][e]));   // (the second channel of a pair: sums of 16 c)
 #pragma unroll
                 for (int m = 2 * j; m < 2 * j + 2; ++m) {
-                    A.a[m][e] = fmaf(A.a[m][e] * LIFT, back, z);
-                    A.a[m][2 + e] = fmaf(A.a[m][2 + e] * (LIFT / 16), back, z);
+                    A.a[m][e] = fmaf(A.a[m][e] * CODE, back, z);
+                    A.a[m][2 + e] = fmaf(A.a[m][2 + e] * (CODE / 16), back, z);
                 }
             }
     }

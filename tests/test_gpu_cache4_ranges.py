@@ -94,3 +94,18 @@ def test_values_small_and_large(size, kind):
             v *= size
         r, (q, k1, v1) = edited(kind, "bf16", *shape[:2], 2, *shape[2:], edit)
         r.step(tokens=(q, k1, (v1.double() * size).to(v1.dtype)), which=[0, 1, shape[0] * shape[1] - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["four accum", "four learned"])
+@pytest.mark.parametrize("power", [117, 110, 60, -60, -110, -117])
+def test_keys_and_queries_of_opposite_size(power, kind, dtype):
+    """Keys 2^power times, queries 2^-power times their ordinary size: logits of the ordinary size."""
+    for shape in SHAPES:
+        for G in (1, 3):
+            def edit(k, v, q):
+                k *= 2.0 ** power
+            r, (q, k1, v1) = edited(kind, dtype, *shape[:2], G, *shape[2:], edit)
+            if r.conv is not None:                             # (a scorer whose logits of such keys are ordinary)
+                r.w[..., :r.s.d] *= 2.0 ** -power
+            r.step(tokens=(q * 2.0 ** -power, k1 * 2.0 ** power, v1), decay=0.9, which=[0, 1, shape[0] * shape[1] - 1])
