@@ -55,6 +55,14 @@ void* ptr(PyObject* o, at::ScalarType type)
     if (o != Py_None && THPVariable_Unpack(o).scalar_type() != type) fail(PyExc_AssertionError, "a tensor has another dtype than the call expects");
     return p;
 }
+// device pointer of a cache that has `need` bytes at least, NULL for None: a call walks all of it (a cache in 4 bits is shorter than an
+// ordinary one)
+void* cache_ptr(PyObject* o, size_t need)
+{
+    void* p = ptr(o);
+    if (o != Py_None && THPVariable_Unpack(o).nbytes() < need) fail(PyExc_ValueError, "the cache is shorter than this shape's");
+    return p;
+}
 float* fptr(PyObject* o) { return (float*)ptr(o, at::kFloat); }
 int32_t* iptr(PyObject* o) { return (int32_t*)ptr(o, at::kInt); }
 
@@ -213,7 +221,7 @@ LTE_FN(cache_init, 8)
     const void *k = ptr(a[2]), *v = ptr(a[3]);
     const float* z = (const float*)ptr(a[4]);
     const int32_t *idx = (const int32_t*)ptr(a[5]), *cnt = (const int32_t*)ptr(a[6]);
-    void* cache = ptr(a[7]);
+    void* cache = cache_ptr(a[7], lte_cache_bytes(s));
     call("lte_cache_init", [&](void* st) { return lte_cache_init(s, c, k, v, z, idx, cnt, cache, st); });
     return Py_NewRef(a[7]);
 }
@@ -224,7 +232,7 @@ LTE_FN(attn_decode, 8)
     const lte_shape* s = c_struct<lte_shape>(a[0]);
     const lte_conv* c = c_struct<lte_conv>(a[1]);
     const at::Tensor& q = tensor(a[3]);
-    void* cache = ptr(a[2]);
+    void* cache = cache_ptr(a[2], lte_cache_bytes(s));
     const void *q1 = ptr(a[3]), *k1 = ptr(a[4]), *v1 = ptr(a[5]);
     Out o(a[6], q.sizes(), q.scalar_type(), q, false), lse(a[7], {s->B, heads_q(s)}, at::kFloat, q);
     call("lte_attn_decode", [&](void* st) { return lte_attn_decode(s, c, cache, q1, k1, v1, o.as<void>(), lse.as<float>(), st); });
@@ -239,7 +247,7 @@ LTE_FN(attn_prefill_chunk, 11)
     const long n_past = PyLong_AsLong(a[3]), flags = PyLong_AsLong(a[10]);
     if (PyErr_Occurred()) throw PyFailure();
     const at::Tensor& q = tensor(a[4]);
-    void* cache = ptr(a[2]);
+    void* cache = cache_ptr(a[2], lte_cache_bytes(s));
     const void *qp = ptr(a[4]), *k = ptr(a[5]), *v = ptr(a[6]);
     Out o(a[7], q.sizes(), q.scalar_type(), q, false), lse(a[8], {s->B, heads_q(s), s->T}, at::kFloat, q);
     Scratch ws(a[9], a[9] == Py_None ? lte_workspace_bytes((flags & LTE_CHUNK_STREAMING) ? LTE_OP_CHUNK_STREAM : LTE_OP_CHUNK, s, c) : 0, q, 256);
@@ -261,7 +269,7 @@ const at::Tensor& cache_tensor(PyObject* o, size_t need)
 {
     const at::Tensor& t = tensor(o);
     ptr(o, at::kByte);
-    if ((size_t)t.numel() < need) fail(PyExc_ValueError, "the cache is shorter than this shape's");
+    cache_ptr(o, need);
     return t;
 }
 at::ScalarType element(const lte_shape* s) { return s->dtype == LTE_BF16 ? at::kBFloat16 : at::kFloat; }
@@ -348,7 +356,7 @@ LTE_FN(cache_score, 6)
     const lte_shape* s = c_struct<lte_shape>(a[0]);
     const lte_conv* c = c_struct<lte_conv>(a[1]);
     const at::Tensor& like = tensor(a[2]);
-    void* cache = ptr(a[2]);
+    void* cache = cache_ptr(a[2], lte_cache_bytes(s));
     const float *co = fptr(a[3]), *si = fptr(a[4]);
     const int32_t len = co ? (int32_t)THPVariable_Unpack(a[3]).size(0) : 0;
     Scratch ws(a[5], a[5] == Py_None ? lte_workspace_bytes(LTE_OP_DECODE, s, c) : 0, like, 256);
