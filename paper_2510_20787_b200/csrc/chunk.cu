@@ -48,6 +48,10 @@ __global__ void chunk_gather_kernel(const unsigned char* __restrict__ cache, Cac
     const int32_t* meta = reinterpret_cast<const int32_t*>(blk + L.off_meta);
     if (meta[0] != n0) {
         if (threadIdx.x == 0) { atomicExch(&g_chunk_status.code, 31); if (blockIdx.x == 0) gate[bh] = 0; }
+        if (blockIdx.x == 0) {                                 // no pool and no logits: what the kernels behind this one go by stays in range
+            for (int r = threadIdx.x; r < R0 + Wn; r += blockDim.x) zsrc[(size_t)bh * (R + W) + r] = -INFINITY;
+            for (int r = threadIdx.x; r < R; r += blockDim.x) oldpos[(size_t)bh * R + r] = -1;
+        }
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) gate[bh] = 1;
