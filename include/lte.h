@@ -10,7 +10,7 @@
  *
  * State the library keeps between calls, all of it per device and none of it results: (1) on the
  * host, a small table per device ordinal, filled on first use under a mutex (SM count, the raised
- * dynamic-shared-memory limits of its kernels, one symbol address), so any number of host threads
+ * dynamic-shared-memory limits of its kernels, two symbol addresses), so any number of host threads
  * may call into the library on any devices; (2) on each device, one status record per kernel
  * family (see lte_device_status) and the fixed scratch array of lte_attn_bwd_static.  Calls act
  * on the device that is current when they are made.
@@ -92,7 +92,7 @@ size_t lte_workspace_bytes(int op, const lte_shape* s, const lte_conv* c);
 /*
  * Sticky device-side status of the current device: LTE_OK, or LTE_ERR_DEVICE_STATUS if, since the last call of this
  * function, a kernel gave up on a bounded wait (the outputs of that launch are undefined) or found its input state other
- * than the call said (lte_attn_prefill_chunk, lte_cache_score_unrope describe their cases).  The record is per DEVICE
+ * than the call said (lte_attn_prefill_chunk, lte_cache_score_unrope, lte_cache_bytes describe the cases).  The record is per DEVICE
  * (one word per kernel family), not per cache, workspace or stream: with several caches or streams in flight it tells
  * that something went wrong on the device, not whose launch it was; synchronise and check after the call you care
  * about.  Only the launch that recorded an anomaly is affected: launches made after it, before or after the status is
@@ -199,6 +199,12 @@ int lte_attn_prefill(const lte_shape* s, const void* q, const void* k, const voi
  * rows_alloc = W+R, except for bf16 with d = 64 and W+R <= 256, where rows_alloc = 256 (zero rows at the end) and each
  * key/value row is stored with the 128-byte swizzle (16-byte chunk c of row r sits at chunk position c ^ (r & 7)),
  * which is the layout the tensor-core decode kernel consumes directly from shared memory.
+ *
+ * The header's first word says what a cache holds: 0 (lte_cache_init) stands for logits, 0x4c544501 for accumulated attention in their place
+ * (lte_cache_init_accum), 0x4c544502 and 0x4c544503 for the same in 4 bits (lte_cache4_pack); any other value says nothing.  A call
+ * that finds by it a cache which it cannot read records that (lte_device_status): lte_attn_prefill_chunk, lte_cache_score and the
+ * decode steps on accumulated attention or 4 bits leave the cache (and, the steps, o1 and lse1) as it was; after lte_attn_decode (which in fp32 with
+ * one query head per key/value head does not look) and lte_cache4_unpack what they write is undefined.
  */
 size_t lte_cache_bytes(const lte_shape* s);
 
@@ -251,8 +257,8 @@ int lte_attn_decode(const lte_shape* s, const lte_conv* c, void* cache,
  *   a        in   [B,H,T] fp32 (idx, cnt as written by lte_select_rule)
  *   decay    0 .. 1
  *   cache    in/out;   q1, k1, v1, o1, lse1 as for lte_attn_decode
- * Deterministic.  A score that is NaN (of a head whose logits were) ranks above every number.  A cache in this state does not go through the calls that read logits (lte_attn_decode, lte_attn_prefill_chunk,
- * lte_cache_score): they would take a for logits.
+ * Deterministic.  A score that is NaN (of a head whose logits were) ranks above every number.  The calls that read logits (lte_attn_decode,
+ * lte_attn_prefill_chunk, lte_cache_score) do not take a cache in this state, nor what lte_cache4_unpack makes of it; its header says so to them.
  * Errors: INVALID_ARG (decay outside 0 .. 1), UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
  */
 int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const float* a, const int32_t* idx,
@@ -275,7 +281,7 @@ int lte_attn_decode_accum(const lte_shape* s, float decay, void* cache, const vo
  * the values' 2-byte unit u channels 4g .. 4g+3 of group u mod (d/32), g = u / (d/32).
  *
  * lte_cache4_pack rounds an ordinary cache (of s->dtype) into 4 bits, lte_cache4_unpack writes the values back into an ordinary cache
- * (bf16: rounded to it), e.g. for lte_attn_prefill_chunk when a conversation goes on; neither changes its input.  Both caches are whole
+ * (bf16: rounded to it), e.g. under the learned rule for lte_attn_prefill_chunk when a conversation goes on; neither changes its input.  Both caches are whole
  * and must not overlap.  lte_cache4_bytes is 0 for a shape that the calls refuse.  s->T is ignored.
  * Errors: INVALID_ARG, UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
  */

@@ -123,12 +123,13 @@ __global__ void __launch_bounds__(PT) cache4_pack_kernel(const unsigned char* __
             if (threadIdx.x == i)
                 for (size_t e = off[i] + len; e < off[i + 1]; e += 4) *reinterpret_cast<uint32_t*>(dst + e) = 0u;
     }
-    if (blockIdx.x == 0 && threadIdx.x < Q.header / 4) reinterpret_cast<uint32_t*>(cache4)[threadIdx.x] = 0u;
+    if (blockIdx.x == 0 && threadIdx.x < Q.header / 4)
+        reinterpret_cast<uint32_t*>(cache4)[threadIdx.x] = threadIdx.x == 0 ? kCacheMark | kCacheFour | cache_holds(cache) : 0u;
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(PT) cache4_unpack_kernel(const unsigned char* __restrict__ cache4, Cache4Layout Q, unsigned char* __restrict__ cache,
-                                                           CacheLayout L, int W, int R, int parts)
+                                                           CacheLayout L, int W, int R, int parts, int* status)
 {
     constexpr int PIECES = D / 8, GROUPS = D / kGroup4;
     pdl_launch_dependents();
@@ -161,7 +162,10 @@ __global__ void __launch_bounds__(PT) cache4_unpack_kernel(const unsigned char* 
         }
     }
     copy_tail(src, Q.off_z, Q.off_pidx, Q.off_meta, dst, L.off_z, L.off_pidx, L.off_meta, L.stride, rows, R, part, parts);
-    if (blockIdx.x == 0 && threadIdx.x < L.header / 4) reinterpret_cast<uint32_t*>(cache)[threadIdx.x] = 0u;
+    const uint32_t holds = blockIdx.x == 0 ? cache_holds(cache4) : 0u;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && holds == kCacheAccum) atomicExch(status, kWrongCache);   // an ordinary cache
+    if (blockIdx.x == 0 && threadIdx.x < L.header / 4)
+        reinterpret_cast<uint32_t*>(cache)[threadIdx.x] = threadIdx.x == 0 && (holds & kCacheAccum) ? kCacheMark | kCacheAccum : 0u;
 }
 
 template <typename F> int by_type(const Params& p, F&& f)      // f(element, head dimension)
@@ -194,9 +198,11 @@ int launch_cache4_unpack(const Params& p, const void* cache4, void* cache, cudaS
     const CacheLayout L = cache_layout(p.d, p.W, p.R, p.dtype);
     const Cache4Layout Q = cache4_layout(p.d, p.W, p.R);
     const int parts = (L.rows_alloc + PROWS - 1) / PROWS;
+    int* status = nullptr;
+    if (int e = cache_status_word(&status)) return e;
     return by_type(p, [&](auto t, auto d) {
         return cuda_status(launch_pdl(cache4_unpack_kernel<decltype(t), decltype(d)::value>, dim3(parts * p.B * p.H), dim3(PT), 0, st,
-                                      (const unsigned char*)cache4, Q, (unsigned char*)cache, L, p.W, p.R, parts)); });
+                                      (const unsigned char*)cache4, Q, (unsigned char*)cache, L, p.W, p.R, parts, status)); });
 }
 
 }  // namespace lte

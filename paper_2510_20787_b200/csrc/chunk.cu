@@ -17,7 +17,7 @@
 
 namespace lte {
 
-__device__ StatusWord g_chunk_status = LTE_STATUS_INIT;   // report only; 31: the cache does not hold n_past tokens
+__device__ StatusWord g_chunk_status = LTE_STATUS_INIT;   // report only; 31: the cache does not hold n_past tokens, kWrongCache
 
 namespace {
 
@@ -31,7 +31,7 @@ constexpr int kRowsPerBlock = 128;
 // chunk's rows of k, v.  Part 0 also copies the logits of the pool and the ring into zsrc [R0 + Wn] and the pool's
 // positions into oldpos [R], and writes gate[b,h] = 1 if the head's cache holds n0 tokens as the call said, else 0 (the
 // head's cache is then left alone by the commit of this same call; the flag lives in the call's scratch, so it says
-// nothing about any other call).
+// nothing about any other call).  The same for a cache whose scores are no logits.
 __global__ void chunk_gather_kernel(const unsigned char* __restrict__ cache, CacheLayout L, const unsigned char* __restrict__ kc,
                                     const unsigned char* __restrict__ vc, unsigned char* __restrict__ klin,
                                     unsigned char* __restrict__ vlin, float* __restrict__ zsrc, int32_t* __restrict__ oldpos,
@@ -46,8 +46,9 @@ __global__ void chunk_gather_kernel(const unsigned char* __restrict__ cache, Cac
     const float* zc = reinterpret_cast<const float*>(blk + L.off_z);
     const int32_t* pidx = reinterpret_cast<const int32_t*>(blk + L.off_pidx);
     const int32_t* meta = reinterpret_cast<const int32_t*>(blk + L.off_meta);
-    if (meta[0] != n0) {
-        if (threadIdx.x == 0) { atomicExch(&g_chunk_status.code, 31); if (blockIdx.x == 0) gate[bh] = 0; }
+    const bool wrong = cache_holds(cache) != 0u;
+    if (meta[0] != n0 || wrong) {
+        if (threadIdx.x == 0) { atomicExch(&g_chunk_status.code, wrong ? kWrongCache : 31); if (blockIdx.x == 0) gate[bh] = 0; }
         if (blockIdx.x == 0) {                                 // no pool and no logits: what the kernels behind this one go by stays in range
             for (int r = threadIdx.x; r < R0 + Wn; r += blockDim.x) zsrc[(size_t)bh * (R + W) + r] = -INFINITY;
             for (int r = threadIdx.x; r < R; r += blockDim.x) oldpos[(size_t)bh * R + r] = -1;
@@ -345,6 +346,14 @@ int launch_chunk_stream(const Params& p, const float* zrank, const int32_t* oldp
     return cuda_status(cudaGetLastError());
 }
 
+int cache_status_word(int** code)
+{
+    static PerDevice<void*> table;
+    void* at = nullptr;
+    if (int e = table.get(&at, [](void** out) { return cuda_status(cudaGetSymbolAddress(out, g_chunk_status)); })) return e;
+    *code = &static_cast<StatusWord*>(at)->code;
+    return LTE_OK;
+}
 int chunk_status_fetch_and_clear() { return status_fetch_and_clear(g_chunk_status); }
 
 // p.T = local length; the launchers run on one stream in the order gather, (scores), merge, (select, attention), commit

@@ -59,7 +59,7 @@ struct CacheLayout {
     size_t off_pidx;       // [R] int32 positions of pool entries
     size_t off_meta;       // int32[4]: n (tokens seen), cnt (pool entries), reserved x2
     size_t stride;         // bytes per (b,h), multiple of 256
-    size_t header;         // bytes before the first (b,h) block (status word lives at byte 0)
+    size_t header;         // bytes before the first (b,h) block (the first word says what the cache holds, see kCacheAccum)
     int rows_alloc;        // key/value rows per block (W+R, or 256 with zero rows at the end in the swizzled layout)
     int swz;               // 1: bf16, d = 64, W+R <= 256: rows are stored with the 128-byte swizzle (16-byte chunk c of
                            //    row r sits at chunk position c ^ (r & 7)) so that the block, once copied to shared memory,
@@ -81,6 +81,16 @@ __host__ __device__ inline CacheLayout cache_layout(int d, int W, int R, int dty
     L.header = 256;
     return L;
 }
+// What a cache holds, in the header's first word: kCacheMark and bits; anything else (0 as lte_cache_init writes it, or a header that the caller wrote)
+// stands for rows and logits, or says nothing.  A call that finds what it cannot read reports kWrongCache.
+constexpr uint32_t kCacheMark = 0x4c544500u, kCacheAccum = 1u, kCacheFour = 2u;   // the scores are accumulated attention; the rows are held in 4 bits
+constexpr int kWrongCache = 33;
+__device__ __forceinline__ uint32_t cache_holds(const void* cache)
+{
+    const uint32_t x = *static_cast<const uint32_t*>(cache);
+    return (x & ~(kCacheAccum | kCacheFour)) == kCacheMark ? x & (kCacheAccum | kCacheFour) : 0u;
+}
+int cache_status_word(int** code);        // where the current device's kernels report it (the chunk kernels' record)
 // chunk position of logical 16-byte chunk `c` of row `row` (bf16, d = 64: 8 chunks per row)
 __host__ __device__ inline int cache_chunk_pos(const CacheLayout& L, int row, int c) { return L.swz ? (c ^ (row & 7)) : c; }
 
@@ -120,7 +130,7 @@ int launch_prefill_tc_pair(const Params& p, const void* q, const void* k, const 
 int prefill_pair_status_fetch_and_clear();
 int prefill_long_status_fetch_and_clear();
 int launch_cache_init(const Params& p, const void* k, const void* v, const float* z, const int32_t* idx,
-                      const int32_t* cnt, void* cache, cudaStream_t st);
+                      const int32_t* cnt, void* cache, uint32_t mark, cudaStream_t st);
 int launch_ring_linearize(const Params& p, const void* cache, void* klin, void* vlin, const float* rope_cos, const float* rope_sin,
                           int rope_len, cudaStream_t st);
 int launch_ring_scatter_z(const Params& p, void* cache, const float* zlin, cudaStream_t st);

@@ -21,6 +21,11 @@ constexpr int DT = 256;           // threads per block
 constexpr int MAX_ROWS = 4096;    // W + R limit of the decode kernel (logits live in shared memory)
 constexpr int NCH = 8;            // 16-byte chunks a thread keeps in flight per tensor
 
+__device__ StatusWord g_decode_status = LTE_STATUS_INIT;   // report only: no wait polls it
+// by one thread: a cache whose scores are no logits, or whose rows are held in 4 bits.  (Not in the fp32 steps of one query head: wherever it stood, the
+// compiler gave those kernels fewer registers, 32 heads x 256 rows 7.2 -> 7.6 us, 16 x 2,000 24.2 -> 26.0 and more.)
+__device__ __forceinline__ void report_cache(const unsigned char* cache) { if (cache_holds(cache) != 0u) atomicExch(&g_decode_status.code, kWrongCache); }
+
 template <typename T> struct V16 { static constexpr int N = 16 / sizeof(T); };
 
 template <typename T> __device__ __forceinline__ void unpack(const uint4& u, float* f);
@@ -287,7 +292,6 @@ __global__ void __launch_bounds__(DT) decode_kernel(unsigned char* __restrict__ 
 // key buffer is refilled with head i+1's keys, and after the PV pass the value buffer is refilled likewise, so
 // the loads of the next head run under the softmax / PV / write-back of the current one.  Everything is computed
 // out of shared memory; only the rows that change go back to HBM.  Used when a block fits (it does at W+R = 256).
-__device__ StatusWord g_decode_status = LTE_STATUS_INIT;   // report only: no wait polls it
 #ifdef LTE_PROFILE
 __device__ long long g_dprof[64];
 #define DPROF(slot) do { if (blockIdx.x == 7 && threadIdx.x == 96 && it == 2) g_dprof[slot] = clock64(); } while (0)
@@ -641,7 +645,7 @@ template <typename U>
 __global__ void __launch_bounds__(256) cache_init_kernel(unsigned char* __restrict__ cache, CacheLayout L, const U* __restrict__ k,
                                                          const U* __restrict__ v, const float* __restrict__ z,
                                                          const int32_t* __restrict__ idx, const int32_t* __restrict__ cnt, int Tlen,
-                                                         int pshift, int W, int R, int half, int parts)
+                                                         int pshift, int W, int R, int half, int parts, uint32_t mark)
 {
     __shared__ int s_pos[IROWS];                               // token of each row of this part, -1: none
     pdl_launch_dependents();
@@ -672,7 +676,7 @@ __global__ void __launch_bounds__(256) cache_init_kernel(unsigned char* __restri
         uint32_t* tail = reinterpret_cast<uint32_t*>(blk + L.off_meta);
         const int n_tail = (int)((L.stride - L.off_meta) / 4);
         for (int e = tid; e < n_tail; e += 256) tail[e] = e == 0 ? (uint32_t)Tlen : e == 1 ? (uint32_t)n_ret : 0u;
-        if (bh == 0 && tid < (int)(L.header / 4)) reinterpret_cast<uint32_t*>(cache)[tid] = 0u;
+        if (bh == 0 && tid < (int)(L.header / 4)) reinterpret_cast<uint32_t*>(cache)[tid] = tid == 0 ? mark : 0u;
     }
     __syncthreads();
     uint4* Kc = reinterpret_cast<uint4*>(blk + L.off_k);
@@ -698,14 +702,14 @@ __global__ void __launch_bounds__(256) cache_init_kernel(unsigned char* __restri
 int decode_status_fetch_and_clear() { return status_fetch_and_clear(g_decode_status); }
 
 int launch_cache_init(const Params& p, const void* k, const void* v, const float* z, const int32_t* idx,
-                      const int32_t* cnt, void* cache, cudaStream_t st)
+                      const int32_t* cnt, void* cache, uint32_t mark, cudaStream_t st)
 {
     const CacheLayout L = cache_layout(p.d, p.W, p.R, p.dtype);
     const int parts = (L.rows_alloc + IROWS - 1) / IROWS;
     auto go = [&](auto unit) {
         using U = decltype(unit);
         return cuda_status(launch_pdl(cache_init_kernel<U>, dim3(parts * p.B * p.H), dim3(256), 0, st, (unsigned char*)cache, L, (const U*)k, (const U*)v,
-                                      z, idx, cnt, p.T, piece_shift(L, p.d), p.W, p.R, p.half, parts));
+                                      z, idx, cnt, p.T, piece_shift(L, p.d), p.W, p.R, p.half, parts, mark));
     };
     // views of k and v may start at any element; from there on their rows are whole pieces
     if ((((uintptr_t)k | (uintptr_t)v) & 15u) == 0) return go(uint4());
@@ -748,6 +752,7 @@ __global__ void __launch_bounds__(256) ring_linearize_kernel(const unsigned char
     const uint4* Kc = reinterpret_cast<const uint4*>(blk + L.off_k);
     const uint4* Vc = reinterpret_cast<const uint4*>(blk + L.off_v);
     const int n = reinterpret_cast<const int32_t*>(blk + L.off_meta)[0];
+    if (blockIdx.x == 0 && threadIdx.x == 0) report_cache(cache);
     const int base = n > W ? n - W : 0, n_eff = n < W ? n : W;
     const int r0 = part * LROWS, n_rows = min(LROWS, W - r0);
     const int hshift = pshift - 1, hp = 1 << hshift;           // pieces of half a row
@@ -797,6 +802,7 @@ __global__ void ring_scatter_z_kernel(unsigned char* __restrict__ cache, CacheLa
     pdl_launch_dependents();
     pdl_wait();
     const int bh = blockIdx.x;
+    if (cache_holds(cache) != 0u) return;                      // (the scores are no logits: reported by the kernel before)
     unsigned char* blk = cache + L.header + (size_t)bh * L.stride;
     float* zc = reinterpret_cast<float*>(blk + L.off_z);
     const int n = reinterpret_cast<const int32_t*>(blk + L.off_meta)[0];
@@ -845,6 +851,7 @@ __device__ __forceinline__ void cache_update_block(unsigned char* __restrict__ c
     int32_t* pidx = reinterpret_cast<int32_t*>(blk + L.off_pidx);
     int32_t* meta = reinterpret_cast<int32_t*>(blk + L.off_meta);
     const int n = meta[0], cnt_old = meta[1];
+    if (bh == 0 && tid == 0) report_cache(cache);
     const int slot = n % W, p = n - W, half = K / 2;
 
     // ---- the token leaving the window is offered to the pool (same rule as the step kernels) ----

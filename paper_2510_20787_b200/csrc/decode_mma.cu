@@ -101,7 +101,8 @@ template <int D, int NW, bool SWZ, bool BACK>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_mma_kernel(
     unsigned char* __restrict__ cache, CacheLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, const float* __restrict__ cw,
-    const float* __restrict__ cbias, int H, int W, int R, int sink, int K, float zthr, float scale, int G)
+    const float* __restrict__ cbias, int H, int W, int R, int sink, int K, float zthr, float scale, int G,
+    int* __restrict__ status)
 {
     constexpr int NT = NW * 32, KP = D / 32, MT = D / 16, PITCH = D + 8, PIECES = D / 8, CPL = D / 32;
     constexpr int NBUF = 2;                                    // spans in flight per warp
@@ -129,6 +130,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_mma_kern
     // Everything whose address is known is asked for at once, then everything that needs the counters: two memory latencies
     // stand before the first product, whatever the shape.
     const int n = meta[0], cnt_old = meta[1];
+    const bool wrong = blockIdx.x == 0 && cache_holds(cache) != 0u;   // scores that are no logits, rows in 4 bits
     uint4 qf[KP];                                              // pieces t, t + 4, .. of query head g (of the first pass)
     auto load_q = [&](int g0) {
 #pragma unroll
@@ -167,6 +169,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D) / NW) decode_mma_kern
     auto has = [&](int i) { return BACK ? (unsigned)i < (unsigned)rows.spans : i < rows.spans; };
     Group<D, SWZ> buf[NBUF];
     const float zp = p >= 0 && R > 0 ? zc[slot] : 0.f;
+    if (wrong && tid == 0) atomicExch(status, kWrongCache);
     if (has(first)) { const Span sp = rows.span(first); buf[0].load_k(rows, sp, g, t); buf[0].load_v(rows, sp, g, t); }
     const int jsc = K > 0 ? n - half : -1;                     // K = 0: the scorer runs outside (lte_cache_score)
     auto tap_rows = [&](int tap, float (&kx)[CPL], float (&vx)[CPL]) {   // channels lane, lane + 32, .. of the row under a tap
@@ -439,9 +442,11 @@ int launch_decode_mma(const Params& p, void* cache, const void* q1, const void* 
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = nsplit > 1 ? 2 : 1;
+    int* status = nullptr;
+    if (int e = cache_status_word(&status)) return e;
     auto go = [&](auto kern) {
         return cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
-                                  (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, p.w, p.bias, p.H, p.W, p.R, p.sink, p.K, p.zthr, p.scale, p.G);
+                                  (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, p.w, p.bias, p.H, p.W, p.R, p.sink, p.K, p.zthr, p.scale, p.G, status);
     };
 #define LTE_GO2(D, S, T) (nw == 8 ? go(decode_mma_kernel<D, max_warps(D), S, T>) : nw == 4 ? go(decode_mma_kernel<D, 4, S, T>) : \
                           nw == 3 ? go(decode_mma_kernel<D, 3, S, T>) : nw == 2 ? go(decode_mma_kernel<D, 2, S, T>) : go(decode_mma_kernel<D, 1, S, T>))

@@ -82,7 +82,7 @@ template <int D, int QP, bool FOUR, bool ACCUM>                // QP: query head
 __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restrict__ cache, RowsLayout L, const float* __restrict__ q1,
                                                          const float* __restrict__ k1, const float* __restrict__ v1, float* __restrict__ o1,
                                                          float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink, float scale, int G,
-                                                         int most)                       // most: rows a block may have
+                                                         int most, int* __restrict__ status)   // most: rows a block may have
 {
     using Row = Held<D, FOUR>;
     constexpr int E = Row::E, LPR = Row::LPR, RPP = DT / LPR, NW = DT / 32;
@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
     pdl_launch_dependents();
     pdl_wait();
 
+    const bool wrong = wrong_cache<FOUR, ACCUM>(cache_holds(cache));
     const int n = max(meta[0], 0), cnt_old = min(max(meta[1], 0), R), slot = n % W, p = n - W;
     for (int c = tid; c < D; c += DT) { s_kn[c] = k1[(size_t)bh * D + c]; s_vn[c] = v1[(size_t)bh * D + c]; }
 
@@ -266,6 +267,10 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
         }
         // ---- the cluster's blocks meet -----------------------------------------------------------------------------
         cluster.sync();
+        if (wrong) {                                           // (every block of the launch; nothing has been written yet)
+            if (blockIdx.x == 0 && tid == 0) atomicExch(status, kWrongCache);
+            return;
+        }
         float top[QP], tot[QP];
 #pragma unroll
         for (int g = 0; g < QP; ++g) {
@@ -380,8 +385,9 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
     if (p.dtype == LTE_BF16)
         return four ? launch_decode_rows4_bf16(p, accum, rule, cache, q1, k1, v1, o1, lse1, st) : launch_decode_rows_bf16(p, rule, cache, q1, k1, v1, o1, lse1, st);
     const RowsLayout L = four ? rows_layout(cache4_layout(p.d, p.W, p.R)) : rows_layout(cache_layout(p.d, p.W, p.R, p.dtype));
-    int n_sm = 0;
+    int n_sm = 0, *status = nullptr;
     if (int e = device_sm_count(&n_sm)) return e;
+    if (int e = cache_status_word(&status)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R;
     auto go = [&](auto d, auto qp, auto f4, auto acc) {
         constexpr int D = decltype(d)::value, QP = decltype(qp)::value;
@@ -402,7 +408,7 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
         attr[1].val.clusterDim.x = nsplit; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = nsplit > 1 ? 2 : 1;
         return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const float*)q1, (const float*)k1, (const float*)v1, (float*)o1, lse1,
-                                              rule, p.H, p.W, p.R, p.sink, p.scale, p.G, (rows + nsplit - 1) / nsplit));
+                                              rule, p.H, p.W, p.R, p.sink, p.scale, p.G, (rows + nsplit - 1) / nsplit, status));
     };
     auto kinds = [&](auto d, auto qp) {
         if (!four) return go(d, qp, std::false_type(), std::true_type());   // (the learned rule over ordinary caches is lte_attn_decode)

@@ -21,6 +21,12 @@ struct RowsRule {
     const float *w, *bias;
 };
 
+// A cache that a step cannot read: of the other width, or attention sums where it reads logits.  (A cache without a mark is what the caller says.)
+template <bool FOUR, bool ACCUM> __device__ __forceinline__ bool wrong_cache(uint32_t holds)
+{
+    return !FOUR ? (holds & kCacheFour) != 0u : ACCUM ? holds == kCacheAccum : (holds & kCacheAccum) != 0u;
+}
+
 // The pool's worst entry: lowest score, the youngest among equals.  As a key whose minimum is wanted and the position to break ties.
 struct Worst {
     uint32_t key = 0xffffffffu;

@@ -393,7 +393,7 @@ template <int D, int NW, int STAGES, bool SWZ, bool FOUR, int RULE>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
-    float scale, int G, int most)                              // most: rows whose logits a warp may have to keep (whole units)
+    float scale, int G, int most, int* __restrict__ status)    // most: rows whose logits a warp may have to keep (whole units)
 {
     using Gr = Group<D, SWZ, FOUR>;
     constexpr bool ACCUM = RULE != LEARNED;
@@ -413,6 +413,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
     __shared__ uint32_t s_wkey[NW];
     __shared__ int s_wpos[NW], s_wslot[NW];
     __shared__ __align__(16) int4 s_worst[SPLIT];
+    __shared__ __align__(16) uint32_t s_holds[4];              // the cache's header
     cg::cluster_group cluster = cg::this_cluster();
     const int nsplit = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int bh = blockIdx.x / nsplit, h = bh % H;
@@ -487,6 +488,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         sv = {rows.V + (size_t)first * (UR * St::ROW) + 16 * lane, rows.VP + (size_t)first * P + 16 * lane, first};
         fill(0);
     };
+    if (tid == 0) tc::cp_async16(tc::smem_u32(s_holds), cache, 16);
     begin();
     const int n = max(n_held, 0), cnt_old = min(max(cnt_held, 0), R);
     typename Gr::Query qf;
@@ -788,6 +790,11 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
         Gr::finish(acc);
         __syncthreads();                                       // the incoming token is there; the previous pass has been combined
+        if (g0 == 0 && wrong_cache<FOUR, ACCUM>(cache_holds(s_holds))) {   // (every block of the launch; nothing has been written yet)
+            if (shared_head && !met) cluster.barrier_wait();
+            if (blockIdx.x == 0 && tid == 0) atomicExch(status, kWrongCache);
+            return;
+        }
         if (wid == 0 && g == 0) { s_unit[2 * t] = qf.unit[0]; s_unit[2 * t + 1] = qf.unit[1]; }
         if (g == 0) { s_m[wid][2 * t] = m0; s_m[wid][2 * t + 1] = m1; s_l[wid][2 * t] = l0; s_l[wid][2 * t + 1] = l1; }
 #pragma unroll
@@ -996,8 +1003,9 @@ template <bool FOUR, bool ACCUM>
 int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1,
                     void* o1, float* lse1, cudaStream_t st)
 {
-    int n_sm = 0;
+    int n_sm = 0, *status = nullptr;
     if (int e = device_sm_count(&n_sm)) return e;
+    if (int e = cache_status_word(&status)) return e;
     const int BH = p.B * p.H, rows = p.W + p.R, wps = warps_per_sm(p.d, FOUR), warps = wps * n_sm;
     const int UR = FOUR || p.d < 128 ? 32 : 16;                // rows that a warp takes at a time (Stage::UR)
     // Long rows of few heads take more warps and blocks: 8 heads x 17,408 rows at d = 128, four query heads each, take 39.5 us with four warps,
@@ -1077,7 +1085,7 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
             cfg.attrs = attr; cfg.numAttrs = split > 1 ? 2 : 1;
             return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
                                                   (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
-                                                  ((rows + UR - 1) / UR + nw * split - 1) / (nw * split) * UR));
+                                                  ((rows + UR - 1) / UR + nw * split - 1) / (nw * split) * UR, status));
         };
         auto with = [&](auto stages) {
             if constexpr (!ACCUM) return with_kind(stages, std::integral_constant<int, LEARNED>());

@@ -174,6 +174,8 @@ __global__ void __launch_bounds__(kThreads<NC>, kPerSm<NC>) decode_tc_kernel(uns
                 }
             }
         }
+        __syncwarp();                                          // (behind the control lane's work)
+        if (blockIdx.x == 0 && lane == 1 && cache_holds(cache) != 0u) atomicExch(&g_decode_tc_status.code, kWrongCache);   // scores that are no logits, rows in 4 bits
     } else {
         // ======================================== compute threads ===============================================
         // Warp-per-row pieces: a lane has channels 2 lane, 2 lane + 1.  The inputs of a head are fetched under the head before.

@@ -341,7 +341,7 @@ int lte_cache_init(const lte_shape* s, const lte_conv* c, const void* k, const v
     if (s->T > 0 && (!k || !v || !z || !cnt || (s->R > 0 && !idx))) return LTE_ERR_INVALID_ARG;
     if (!aligned(k, element_bytes(s)) || !aligned(v, element_bytes(s))) return LTE_ERR_INVALID_ARG;
     e = check_arch(); if (e) return e;
-    return launch_cache_init(make_params(s, c), k, v, z, idx, cnt, cache, (cudaStream_t)stream);
+    return launch_cache_init(make_params(s, c), k, v, z, idx, cnt, cache, 0u, (cudaStream_t)stream);
 }
 
 int lte_cache_score(const lte_shape* s, const lte_conv* c, void* cache, void* ws, size_t ws_bytes, void* stream)
@@ -457,7 +457,7 @@ int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const
     if (s->T > 0 && (!k || !v || !a || !cnt || (s->R > 0 && !idx))) return LTE_ERR_INVALID_ARG;
     if (!aligned(k, element_bytes(s)) || !aligned(v, element_bytes(s))) return LTE_ERR_INVALID_ARG;
     e = check_arch(); if (e) return e;
-    return launch_cache_init(make_params(s, nullptr), k, v, a, idx, cnt, cache, (cudaStream_t)stream);   // (no token is unscored)
+    return launch_cache_init(make_params(s, nullptr), k, v, a, idx, cnt, cache, kCacheMark | kCacheAccum, (cudaStream_t)stream);   // (no token is unscored)
 }
 
 static int decode_rows(const lte_shape* s, const lte_conv* c, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1,

@@ -219,7 +219,8 @@ def lte_cache_init_accum(s, k=None, v=None, a=None, idx=None, cnt=None, cache=No
 
 def lte_attn_decode_accum(s, cache, q1, k1, v1, decay=1.0, o1=None, lse1=None):
     """One decode step under eviction by accumulated attention: q1 [B,H*group,d], k1, v1 [B,H,d] -> o1 [B,H*group,d], lse1
-    [B,H*group]; the cache of lte_cache_init_accum is updated in place, its scores to decay * score + this step's weights."""
+    [B,H*group]; the cache of lte_cache_init_accum is updated in place, its scores to decay * score + this step's weights.  (The calls that read
+    logits do not take it: lte_attn_decode, lte_attn_prefill_chunk, lte_cache_score.)"""
     return (_native or _load()).attn_decode_rows(s, None, float(decay), cache, q1, k1, v1, o1, lse1, False)
 
 
@@ -236,7 +237,8 @@ def lte_cache4_pack(s, cache, cache4=None):
 
 
 def lte_cache4_unpack(s, cache4, cache=None):
-    """A cache in 4 bits as an ordinary one of s.dtype, e.g. for lte_attn_prefill_chunk."""
+    """A cache in 4 bits as an ordinary one of s.dtype, e.g. (learned rule) for lte_attn_prefill_chunk.  Scores stay what they were: the sums of
+    attention of a cache of lte_cache_init_accum are no logits, and the calls that read those do not take it."""
     if cache is None:
         cache = _new_cache("lte_cache4_unpack", lte_cache_bytes(s), cache4)
     return (_native or _load()).cache4_convert(s, cache4, cache, False)

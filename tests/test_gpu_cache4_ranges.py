@@ -54,12 +54,10 @@ def test_a_row_of_large_values_that_weighs_nothing(shape, power, kind, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["four accum", "four learned"])
 @pytest.mark.parametrize("power", [10, 20, 30, 60])
-@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("shape", [x for x in SHAPES if x[2] > 32])
 def test_groups_of_channels_of_different_size(shape, power, kind, dtype):
     """The first 32 channels of one row, or of every row, 2^power times the others: what the other channels come to does not depend on them."""
     B, H, d, W, R = shape
-    if d == 32:
-        pytest.skip("one group")
     which = [0, 1, B * H - 1]
     for rows in (slice(None), slice(7, 8), slice(W, None)):
         def edit(k, v, q):
