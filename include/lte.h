@@ -282,7 +282,7 @@ int lte_attn_decode_accum(const lte_shape* s, float decay, void* cache, const vo
  *
  * lte_cache4_pack rounds an ordinary cache (of s->dtype) into 4 bits, lte_cache4_unpack writes the values back into an ordinary cache
  * (bf16: rounded to it), e.g. under the learned rule for lte_attn_prefill_chunk when a conversation goes on; neither changes its input.  Both caches are whole
- * and must not overlap.  lte_cache4_bytes is 0 for a shape that the calls refuse.  s->T is ignored.
+ * and must not overlap.  lte_cache4_bytes is 0 for a shape that the calls refuse.  s->T and s->tau are ignored.
  * Errors: INVALID_ARG, UNSUPPORTED (W + R > 32768, d not in {32,64,128}), CUDA.
  */
 size_t lte_cache4_bytes(const lte_shape* s);

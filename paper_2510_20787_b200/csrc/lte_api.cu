@@ -102,12 +102,22 @@ int check_conv_or_stack(const lte_shape* s, const lte_conv* c)
     return check_conv(s, c);
 }
 
+// the shape of a call that has no threshold: tau is ignored
+int check_shape_no_tau(const lte_shape* s, bool need_T)
+{
+    if (!s) return LTE_ERR_INVALID_ARG;
+    lte_shape one = *s;
+    one.tau = 0.f;
+    return check_shape(&one, need_T);
+}
+
 // shapes of the calls on caches that evict by accumulated attention or hold 4 bits
-int check_rows(const lte_shape* s)
+int check_rows(const lte_shape* s, bool threshold = false)
 {
     if (!s) return LTE_ERR_INVALID_ARG;
     lte_shape one = *s;
     one.T = 0;                                               // (ignored)
+    if (!threshold) one.tau = 0.f;                           // (ignored)
     if (int e = check_shape(&one, false)) return e;
     if ((long long)s->W + s->R > kRowsMost) return LTE_ERR_UNSUPPORTED;
     if ((double)s->B * s->H * ((double)s->W + s->R) > 2.0e9) return LTE_ERR_UNSUPPORTED;   // blocks of a launch
@@ -287,7 +297,7 @@ int lte_select_rule(const lte_shape* s, int rule, const float* score, int32_t* i
                     void* ws, size_t ws_bytes, void* stream)
 {
     if (rule == LTE_RULE_LEARNED) return lte_select(s, score, idx, cnt, ncand_or_null, ws, ws_bytes, stream);
-    int e = check_shape(s, true); if (e) return e;
+    int e = check_shape_no_tau(s, true); if (e) return e;
     if (!cnt || (s->R > 0 && !idx)) return LTE_ERR_INVALID_ARG;
     if (s->T - s->W > (1 << 24)) return LTE_ERR_UNSUPPORTED;
     if (rule == LTE_RULE_UNIFORM) {
@@ -451,7 +461,7 @@ int lte_attn_decode(const lte_shape* s, const lte_conv* c, void* cache, const vo
 int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const float* a, const int32_t* idx, const int32_t* cnt, void* cache,
                          void* stream)
 {
-    int e = check_shape(s, false); if (e) return e;
+    int e = check_shape_no_tau(s, false); if (e) return e;
     e = check_rows(s); if (e) return e;
     if (!cache || !aligned16(cache)) return LTE_ERR_INVALID_ARG;
     if (s->T > 0 && (!k || !v || !a || !cnt || (s->R > 0 && !idx))) return LTE_ERR_INVALID_ARG;
@@ -463,7 +473,7 @@ int lte_cache_init_accum(const lte_shape* s, const void* k, const void* v, const
 static int decode_rows(const lte_shape* s, const lte_conv* c, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1,
                        const void* v1, void* o1, float* lse1, void* stream)
 {
-    int e = check_rows(s); if (e) return e;
+    int e = check_rows(s, !accum); if (e) return e;
     if (accum) {
         if (!(decay >= 0.f && decay <= 1.f)) return LTE_ERR_INVALID_ARG;
     } else {
