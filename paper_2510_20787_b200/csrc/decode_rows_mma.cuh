@@ -78,9 +78,9 @@ template <int D, bool FOUR> struct Stage {
 // N 4-byte words of shared memory (one load; from reinterpreted pointers the compiler makes single words)
 template <int N> __device__ __forceinline__ void lds(uint32_t (&x)[N], uint32_t at)
 {
-    if constexpr (N == 1) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(at));
-    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(at));
-    else asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at));
+    if constexpr (N == 1) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x[0]) : "r"(at) : "memory");
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(at) : "memory");
+    else asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(at) : "memory");
 }
 
 // The two products with a span of 16 rows that stands in shared memory, lane (g, t) = (lane / 4, lane % 4).  Rows past the last one and those that the
@@ -347,7 +347,7 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
         for (int u = 0; u < 4; ++u) {
             if constexpr (GR == 1) {                           // M-rows 2t + (u & 1) + 8 (u / 2)
                 uint16_t x;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(values + u * (2 * D)));
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(values + u * (2 * D)) : "memory");
                 v[u][0] = x;
             } else {
                 lds(v[u], values + u * (2 * D));
