@@ -274,6 +274,24 @@ const at::Tensor& cache_tensor(PyObject* o, size_t need)
 }
 at::ScalarType element(const lte_shape* s) { return s->dtype == LTE_BF16 ? at::kBFloat16 : at::kFloat; }
 
+// The tensors behind a scorer, which lte.conv keeps with the struct (one that the caller filled in by hand has none): all heads' weights, where the
+// cache is.
+void check_scorer(PyObject* o, const lte_conv* c, const lte_shape* s, const at::Tensor& cache)
+{
+    PyObject* keep = PyObject_GetAttrString(o, "_keep");
+    if (!keep) { PyErr_Clear(); return; }
+    bool fits = true;
+    if (c->n_layers == 1 && PyTuple_Check(keep))
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(keep); ++i) {
+            PyObject* x = PyTuple_GET_ITEM(keep, i);           // weights [H, K, 2d], bias [H] or None
+            if (!THPVariable_Check(x)) continue;
+            const at::Tensor& t = THPVariable_Unpack(x);
+            fits = fits && t.device() == cache.device() && t.numel() == (int64_t)s->H * (i == 0 ? (int64_t)c->kernel * 2 * s->d : 1);
+        }
+    Py_DECREF(keep);
+    if (!fits) fail(PyExc_ValueError, "the scorer's weights: another size than this shape's, or on another device than the cache");
+}
+
 // s, k, v, a, idx, cnt, cache
 LTE_FN(cache_init_accum, 7)
 {
@@ -305,6 +323,7 @@ LTE_FN(attn_decode_rows, 10)
     if (PyErr_Occurred()) throw PyFailure();
     const bool four = a[9] == Py_True;
     const at::Tensor& cache = cache_tensor(a[3], four ? lte_cache4_bytes(s) : lte_cache_bytes(s));
+    if (c) check_scorer(a[1], c, s, cache);
     const c10::cuda::CUDAGuard guard(cache.device());
     const int64_t heads = (int64_t)s->B * s->H, hq = heads_q(s);
     const at::Tensor& q = on(a[4], cache, s->B * hq * s->d, element(s), "q1: another size or device than the cache's");
