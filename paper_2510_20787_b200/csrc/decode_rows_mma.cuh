@@ -972,7 +972,9 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
 constexpr size_t kMostSmem = 200 * 1024;                       // dynamic, of a block
 
 // The most blocks that a cluster of a head may have so that `heads` of them run at once with one block to an SM; 0 where not even single blocks do.
-// (Clusters lie within a group of SMs, and the groups differ in size: of 148 SMs, 7 clusters of 16 find room, 11 of 10, 15 of 8 or 9, 22 of 6, 33 of 4.)
+// (Clusters lie within a group of SMs, and the groups differ in size: of 148 SMs, 7 clusters of 16 find room, 11 of 10, 15 of 8 or 9, 22 of 6, 33 of 4.
+// Clusters of an odd size, which share pairs of SMs, do not reach their number: of the 26 of 5 and 45 of 3 that the runtime counts, 24 and 44 took up to
+// 23 % longer than the launch without this path (all of them 37 %), three fewer up to 13 % less.)
 template <bool FOUR, bool ACCUM>
 int one_block_an_sm(int heads, int* blocks)
 {
@@ -994,7 +996,7 @@ int one_block_an_sm(int heads, int* blocks)
             }
             return (int)LTE_OK; })) return e;
     *blocks = n.of[MAX_SPLIT] > 0 ? MAX_SPLIT : 8;             // (a launch takes more than 8 only where 16 are possible)
-    while (*blocks > 0 && n.of[*blocks] < heads) --*blocks;
+    while (*blocks > 0 && n.of[*blocks] < heads + (*blocks > 1 && *blocks % 2 ? 3 : 0)) --*blocks;
     return LTE_OK;
 }
 
@@ -1042,13 +1044,14 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     //   d = 64     16 x 17,408   31.1 | 26.8, 19.4 | 23.3       32 x 384   8.2 | 7.9       32 x 1,024   11.3 | 8.4       128 x 1,536   17.0 | 16.1
     // so not 4 bits at d = 64 (32 codes a lane leave 16 warps room).  Not few rows either (8 x 1,024, bf16: 9.9 | 9.1 at d = 128, 7.9 | 8.1 at d = 64;
     // 4 bits accumulated 9.6 | 9.8; 128 x 96, d = 64: 5.8 | 6.1).  Long bf16 rows need many SMs: 64 x 6,024 take 32.8 | 34.4 at d = 128, 20.9 | 22.5
-    // at d = 64, 28 x 17,408 (112 SMs) 50.6 | 54.9, but 40 x 6,024 (120) 29.5 | 25.3.
+    // at d = 64, 28 x 17,408 (112 SMs) 50.6 | 54.9, but 40 x 6,024 (120) 29.5 | 25.3.  One block a head gains up to some 4,000 rows (119 heads x 3,000, d = 128
+    // 37.5 | 36.6, 148 x 3,000 61.3 | 42.6) and loses behind (119 x 8,192, one query head each: 85.6 | 86.9, d = 64 51.1 | 53.6; 148 x 17,408 223 | 233).
     bool wide = false;
     if ((FOUR ? p.d == 128 : p.d >= 64) && rows >= 128 && BH <= n_sm && (long long)BH * rows >= 12288) {
         int c = 0;
         if (int e = one_block_an_sm<FOUR, ACCUM>(BH, &c)) return e;
         const bool fits = !ACCUM || (c > 0 && smem(MAX_WARPS, c) + MAX_WARPS * (FOUR ? 3 * 5 : 2 * 8) * 1024 <= kMostSmem);
-        const bool enough = rows <= 2048 || c >= 6 || (c != 2 && BH * c * 5 >= n_sm * 4);
+        const bool enough = rows <= 2048 || c >= 6 || ((c == 1 ? rows <= 4096 : c != 2) && BH * c * 5 >= n_sm * 4);
         if (c > 0 && (FOUR || (fits && enough))) { wide = true; keep = fits; nw = MAX_WARPS; nsplit = c; }
     }
     auto go = [&](auto d, auto w, auto s) {
