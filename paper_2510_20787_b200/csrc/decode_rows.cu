@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(DT) decode_rows_kernel(unsigned char* __restri
             __syncthreads();
             w.key = lane < NW ? s_wkey[lane] : 0xffffffffu; w.pos = lane < NW ? s_wpos[lane] : -1; w.slot = lane < NW ? s_wslot[lane] : -1;
             w.over_warp();
-            if (w.slot >= 0 && order_key(zp + 0.f) > w.key) dst = w.slot;
+            if (w.slot >= 0 && Worst::rank(zp) > w.key) dst = w.slot;
         }
     }
     const int masked_ring = p >= 0 && dst < 0 ? slot : -1;     // the popped row counts iff the pool takes it ...

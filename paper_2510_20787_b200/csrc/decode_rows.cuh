@@ -31,9 +31,14 @@ template <bool FOUR, bool ACCUM> __device__ __forceinline__ bool wrong_cache(uin
 struct Worst {
     uint32_t key = 0xffffffffu;
     int pos = -1, slot = -1;
+    // -0 counts as 0, NaN of either sign as more than any number (what an addition makes of a NaN's sign is not defined)
+    static __device__ __forceinline__ uint32_t rank(float z)
+    {
+        return (__float_as_uint(z) & 0x7fffffffu) > 0x7f800000u ? 0xffffffffu : order_key(z + 0.f);
+    }
     __device__ __forceinline__ void offer(float z, int at, int m, int sink)
     {
-        const uint32_t k = order_key(z + 0.f);                 // (-0 counts as 0)
+        const uint32_t k = rank(z);
         if (at >= sink && (k < key || (k == key && at > pos))) { key = k; pos = at; slot = m; }
     }
     __device__ __forceinline__ void over_warp()                // every lane then has it

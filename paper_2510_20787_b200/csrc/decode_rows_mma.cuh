@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 w.key = (uint32_t)x.x; w.pos = x.y; w.slot = x.z;
                 w.over_warp();
             }
-            if (w.slot >= 0 && order_key(zp + 0.f) > w.key) dst = w.slot;
+            if (w.slot >= 0 && Worst::rank(zp) > w.key) dst = w.slot;
         }
     }
     const int masked_ring = p >= 0 && dst < 0 ? slot : -32;    // the popped row counts iff the pool takes it ...
