@@ -389,7 +389,13 @@ template <int D, bool SWZ> struct Group<D, SWZ, true> {
 // Where the weights of accumulated attention come from: logits kept in shared memory, or the keys once more (see launch_rows_mma).
 enum { LEARNED = 0, KEPT = 1, AGAIN = 2 };
 
-template <int D, int NW, int STAGES, bool SWZ, bool FOUR, int RULE>
+// LONG: 4 bits, and a warp may have more than kLongRows rows.  Sums of codes are positive and cancel against those of zero; the tensor cores round their
+// running sums towards zero, and after some thousand rows of equal weight that shows (32,768 rows to a warp: 2 % of o).  Every 512 rows what they have
+// then goes to a second sum, which is rounded to the nearest.  It stands in local memory: there are no registers for it, and even so the loop takes
+// up to a fifth longer (256 heads x 1,280 rows, d = 64, accumulated 14.6 -> 17.6 us), which is why it is a variant of its own.
+constexpr int kLongRows = 2048;
+
+template <int D, int NW, int STAGES, bool SWZ, bool FOUR, int RULE, bool LONG>
 __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_rows_mma_kernel(
     unsigned char* __restrict__ cache, RowsLayout L, const __nv_bfloat16* __restrict__ q1, const __nv_bfloat16* __restrict__ k1,
     const __nv_bfloat16* __restrict__ v1, __nv_bfloat16* __restrict__ o1, float* __restrict__ lse1, RowsRule rule, int H, int W, int R, int sink,
@@ -664,6 +670,16 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         const float sq0 = scale2 * qf.unit[0], sq1 = scale2 * qf.unit[1], jump0 = 8.f / sq0, jump1 = 8.f / sq1;
         float m0 = -FLT_MAX, m1 = -FLT_MAX, l0 = 0.f, l1 = 0.f;
         int kept = 0;                                          // rows whose logits this warp has kept
+        volatile float second[MT][4];                          // LONG: the second sums,
+        bool have = false;                                     // whether there is anything in them,
+        int left = 512 / UR;                                   // units until the next
+        auto gather = [&]() {                                  // ... back into the running sums
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc.a[m][e] += second[m][e];
+            have = false;
+        };
 
         const int ring_unit = masked_ring / UR, pool_unit = masked_pool / UR;
         int at_stage = 0;                                      // in bytes
@@ -749,6 +765,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
                 m0 = y0; m1 = y1;
                 l0 *= f0; l1 *= f1;
                 if constexpr (FOUR) {
+                    if constexpr (LONG) { if (have) gather(); }
                     exponentials();
                     Gr::rescale(acc, f0, f1, p, vpar);
                     (void)times_steps();
@@ -761,6 +778,17 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
             for (int x = 0; x < UNIT; ++x) { l0 += p[x][0] + p[x][2]; l1 += p[x][1] + p[x][3]; }
 #pragma unroll
             for (int x = 0; x < UNIT; ++x) Gr::output(acc, p[x], weights[x], vpar[x], st, x, g, t);
+            if constexpr (LONG) {
+                if (--left == 0) {
+                    left = 512 / UR;
+                    if (have) gather();
+                    have = true;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { second[m][e] = acc.a[m][e]; acc.a[m][e] = 0.f; }
+                }
+            }
             __syncwarp();                                      // every lane has read the stage
             if (FOUR) ask_keys(st);
             ask_values(st);
@@ -788,6 +816,7 @@ __global__ void __launch_bounds__(NW * 32, warps_per_sm(D, FOUR) / NW) decode_ro
         if (RULE == KEPT && last) load_old(lane);
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) { l0 += __shfl_xor_sync(0xffffffffu, l0, o); l1 += __shfl_xor_sync(0xffffffffu, l1, o); }
+        if constexpr (LONG) { if (have) gather(); }
         Gr::finish(acc);
         __syncthreads();                                       // the incoming token is there; the previous pass has been combined
         if (g0 == 0 && wrong_cache<FOUR, ACCUM>(cache_holds(s_holds))) {   // (every block of the launch; nothing has been written yet)
@@ -982,7 +1011,7 @@ int one_block_an_sm(int heads, int* blocks)
     static PerDevice<Counts> table;
     Counts n;
     if (int e = table.get(&n, [&](Counts* out) {
-            auto kern = decode_rows_mma_kernel<128, MAX_WARPS, FOUR ? 3 : 2, false, FOUR, ACCUM ? KEPT : LEARNED>;
+            auto kern = decode_rows_mma_kernel<128, MAX_WARPS, FOUR ? 3 : 2, false, FOUR, ACCUM ? KEPT : LEARNED, false>;
             if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem)) return cuda_status(x);
             if (cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) return cuda_status(x);
             for (int c = 1; c <= MAX_SPLIT; ++c) {
@@ -1056,9 +1085,9 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
     }
     auto go = [&](auto d, auto w, auto s) {
         constexpr int D = decltype(d)::value, NW = decltype(w)::value;
-        auto with_kind = [&](auto stages, auto kind) {
+        auto with_length = [&](auto stages, auto kind, auto is_long) {
             constexpr int STAGES = decltype(stages)::value, RULE = decltype(kind)::value;
-            auto kern = decode_rows_mma_kernel<D, NW, STAGES, decltype(s)::value, FOUR, RULE>;
+            auto kern = decode_rows_mma_kernel<D, NW, STAGES, decltype(s)::value, FOUR, RULE, decltype(is_long)::value>;
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute attr[2];
             attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1089,6 +1118,10 @@ int launch_rows_mma(const Params& p, const RowsLayout& L, bool swz, const RowsRu
             return cuda_status(cudaLaunchKernelEx(&cfg, kern, (unsigned char*)cache, L, (const __nv_bfloat16*)q1, (const __nv_bfloat16*)k1,
                                                   (const __nv_bfloat16*)v1, (__nv_bfloat16*)o1, lse1, rule, p.H, p.W, p.R, p.sink, p.scale, p.G,
                                                   ((rows + UR - 1) / UR + nw * split - 1) / (nw * split) * UR, status));
+        };
+        auto with_kind = [&](auto stages, auto kind) {
+            if constexpr (FOUR) { if ((rows + nw * nsplit - 1) / (nw * nsplit) > kLongRows) return with_length(stages, kind, std::true_type()); }
+            return with_length(stages, kind, std::false_type());
         };
         auto with = [&](auto stages) {
             if constexpr (!ACCUM) return with_kind(stages, std::integral_constant<int, LEARNED>());
