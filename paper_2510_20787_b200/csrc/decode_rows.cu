@@ -383,7 +383,7 @@ int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void
 {
     const RowsRule rule = {decay, p.zthr, p.K, p.w, p.bias};
     if (p.dtype == LTE_BF16)
-        return four ? launch_decode_rows4_bf16(p, accum, rule, cache, q1, k1, v1, o1, lse1, st) : launch_decode_rows_bf16(p, rule, cache, q1, k1, v1, o1, lse1, st);
+        return (!four ? launch_decode_rows_bf16 : accum ? launch_decode_rows4_accum_bf16 : launch_decode_rows4_bf16)(p, rule, cache, q1, k1, v1, o1, lse1, st);
     const RowsLayout L = four ? rows_layout(cache4_layout(p.d, p.W, p.R)) : rows_layout(cache_layout(p.d, p.W, p.R, p.dtype));
     int n_sm = 0, *status = nullptr;
     if (int e = device_sm_count(&n_sm)) return e;

@@ -1,11 +1,11 @@
-// What the decode steps of decode_rows.cu (fp32) and decode_rows_mma.cu (bf16) share: eviction by accumulated attention over ordinary
+// What the decode steps of decode_rows.cu (fp32) and decode_rows_mma.cuh (bf16) share: eviction by accumulated attention over ordinary
 // caches, and both eviction rules over caches in 4 bits.
 #pragma once
 #include "cache4.cuh"
 
 namespace lte {
 
-constexpr int kRowsMost = 32768;                               // W + R that the steps take (a row's logits stay in shared memory)
+constexpr int kRowsMost = 32768;                               // W + R that the steps take (fp32: a head's logits stay in the shared memory of eight blocks)
 
 // Where a head's parts stand, whichever way its rows are held.
 struct RowsLayout {
@@ -53,8 +53,10 @@ struct Worst {
 
 int launch_decode_rows_bf16(const Params& p, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
                             cudaStream_t st);
-int launch_decode_rows4_bf16(const Params& p, bool accum, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
-                             float* lse1, cudaStream_t st);
+int launch_decode_rows4_bf16(const Params& p, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1, float* lse1,
+                             cudaStream_t st);
+int launch_decode_rows4_accum_bf16(const Params& p, const RowsRule& rule, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
+                                   float* lse1, cudaStream_t st);
 int launch_decode_rows(const Params& p, bool four, bool accum, float decay, void* cache, const void* q1, const void* k1, const void* v1, void* o1,
                        float* lse1, cudaStream_t st);
 
