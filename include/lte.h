@@ -293,6 +293,8 @@ int lte_cache4_unpack(const lte_shape* s, const void* cache4, void* cache, void*
  * One decode step over a cache in 4 bits: lte_attn_decode (the learned rule; the single-layer scorer, which reads the ring's rows as the
  * cache holds them) and lte_attn_decode_accum.  q1, k1, v1, o1 are of s->dtype; the incoming token is attended and scored as given,
  * and rounded to 4 bits when it takes its ring slot; a row that moves into the pool keeps its codes.
+ * bf16 calls multiply in fp16 on the tensor cores: a weight times its row's step is rounded to 11 bits, under a scale per query head and group of
+ * channels; a query head is held under a scale of its own, in which a channel below 2^-35 of its largest may count as zero.
  * Errors: as lte_attn_decode_accum; the learned rule: INVALID_ARG for what lte_attn_decode refuses in the scorer, UNSUPPORTED for the
  * three-layer stack.
  */
