@@ -7,7 +7,8 @@
 // those lanes: a thread has BATCH rows in flight, and their partial sums for all query heads are added up together, half of them handed to
 // the other half of the lanes in every round (15 shuffles in the place of 64 for four rows, four query heads and 16 lanes).
 // Measured (B200, a step in a CUDA graph; before: a row at a time): 64 heads x 1,280 rows, four query heads each, d = 64 23.0 us (43 MB: 6.6 at 6.56 TB/s),
-// before 39.5; 256 x 256 13.8 us (5.3), before 27.8; 2 heads x 24 rows, d = 32 5.8 us, before 6.3.
+// before 39.5; 256 x 256 13.5 us (5.3), before 27.8; 2 heads x 24 rows, d = 32 5.7 us, before 6.3.  In 4 bits, accumulated | learned: 64 x 1,280 21.0 | 20.5 us
+// (1.1: the same latencies, and eight conversions and multiply-adds a code word), 256 x 256 9.9 | 10.4 (0.9).
 #include <cfloat>
 #include <cooperative_groups.h>
 

@@ -2,8 +2,8 @@
 // operands, as in decode_mma.cu, every query head of a group at once, heads split over warps and clusters where there are few.
 //
 // Bound by memory where rows are bf16; rows in 4 bits are 3.2 times smaller, and there the instructions that unpack and weigh them count for more
-// (about 190 per 16 rows at d = 64, of which the two products' operands are 60, and 2,000 a warp beside them, at 0.55 per cycle: 14 warps an SM do not
-// hide their latencies, and registers for more are not there).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
+// (about 190 per 16 rows at d = 64, of which the two products' operands are 60, and 1,900 a warp beside them, at 0.51 to 0.55 per cycle: 14 warps an SM do
+// not hide their latencies, and registers for more are not there).  Every warp walks units of 16 or 32 rows (interleaved over the warps of all blocks that share the head) that pass
 // through stages of its own in shared memory, keeps its own reference, sum and output, and meets the others once at the end.  The incoming token
 // is no row: its logit is a dot product on the fp32 ALUs, and it joins where the warps meet.
 //
@@ -27,12 +27,13 @@
 //
 // Measured (B200, us a step in a CUDA graph of steps over three caches in turn, full pools; bytes that cannot be avoided at 6.56 TB/s):
 //                                                    accumulated, bf16    4 bits, accumulated    4 bits, learned
-//   2,048 heads x 256 rows, d = 64                       27.7 (21.5)          19.4 (7.2)            19.2 (6.7)
-//   256 x 1,280, four query heads each, d = 64           20.3 (13.3)          14.7 (4.5)            12.8 (4.2)
-//   2,048 x 1,024, d = 64                                 108 (85.3)          58.8 (28.8)           51.9 (26.9)
-//   512 x 1,024, d = 128                                 47.4 (41.9)          28.8 (13.6)
-//   8 x 17,408, four query heads each, d = 128           27.3 (11.1)          19.8 (3.7)            16.5 (3.6)
-//   16 x 1,024, d = 128 (one user)                        8.6 (1.3)            8.7 (0.4)             7.7 (0.4)
+//   2,048 heads x 256 rows, d = 64                       27.8 (21.5)          19.5 (7.2)            19.1 (6.7)
+//   256 x 1,280, four query heads each, d = 64           20.5 (13.3)          14.8 (4.5)            12.9 (4.2)
+//   2,048 x 1,024, d = 64                                 109 (85.3)          58.3 (28.8)           50.7 (26.9)
+//   512 x 1,024, d = 128                                 47.4 (41.9)          28.7 (13.6)           26.7 (13.1)
+//   4,096 x 400, d = 32                                  49.9 (34.7)          37.5 (12.5)           34.7 (11.0)
+//   8 x 17,408, four query heads each, d = 128           27.4 (11.1)          19.5 (3.7)            16.8 (3.6)
+//   16 x 1,024, d = 128 (one user)                        8.8 (1.3)            8.8 (0.4)             7.9 (0.4)
 // Of a step 5 to 8 us are the chain of launch, counters, first rows, meeting and write-back (what 32 rows a head take).  What did not help: 4-bit
 // rows in 80 registers and 24 warps an SM (2,048 x 256: 27.8), bulk copies with a barrier per stage in the place of 16-byte ones (the same for bf16,
 // and 35 instructions per 16 rows more), codes as bf16 numbers 16 + c with P in two terms (1.05 us per 16 rows of 2,048 heads, now 0.67).
