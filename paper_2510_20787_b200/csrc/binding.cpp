@@ -275,7 +275,7 @@ const at::Tensor& cache_tensor(PyObject* o, size_t need)
 at::ScalarType element(const lte_shape* s) { return s->dtype == LTE_BF16 ? at::kBFloat16 : at::kFloat; }
 
 // The tensors behind a scorer, which lte.conv keeps with the struct (one that the caller filled in by hand has none): all heads' weights, where the
-// cache is.
+// cache is.  (More heads than the shape's are there to be left out.)
 void check_scorer(PyObject* o, const lte_conv* c, const lte_shape* s, const at::Tensor& cache)
 {
     PyObject* keep = PyObject_GetAttrString(o, "_keep");
@@ -286,10 +286,10 @@ void check_scorer(PyObject* o, const lte_conv* c, const lte_shape* s, const at::
             PyObject* x = PyTuple_GET_ITEM(keep, i);           // weights [H, K, 2d], bias [H] or None
             if (!THPVariable_Check(x)) continue;
             const at::Tensor& t = THPVariable_Unpack(x);
-            fits = fits && t.device() == cache.device() && t.numel() == (int64_t)s->H * (i == 0 ? (int64_t)c->kernel * 2 * s->d : 1);
+            fits = fits && t.device() == cache.device() && t.numel() >= (int64_t)s->H * (i == 0 ? (int64_t)c->kernel * 2 * s->d : 1);
         }
     Py_DECREF(keep);
-    if (!fits) fail(PyExc_ValueError, "the scorer's weights: another size than this shape's, or on another device than the cache");
+    if (!fits) fail(PyExc_ValueError, "the scorer's weights: fewer than this shape's, or on another device than the cache");
 }
 
 // s, k, v, a, idx, cnt, cache
