@@ -306,7 +306,7 @@ LTE_FN(cache_init_accum, 7)
         k = on(a[1], cache, heads * s->T * s->d, element(s), "k: another size or device than the cache's").data_ptr();
         v = on(a[2], cache, heads * s->T * s->d, element(s), "v: another size or device than the cache's").data_ptr();
         score = (const float*)on(a[3], cache, heads * s->T, at::kFloat, "a: another size or device than the cache's").data_ptr();
-        idx = (const int32_t*)on(a[4], cache, heads * s->R, at::kInt, "idx: another size or device than the cache's").data_ptr();
+        if (s->R > 0) idx = (const int32_t*)on(a[4], cache, heads * s->R, at::kInt, "idx: another size or device than the cache's").data_ptr();
         cnt = (const int32_t*)on(a[5], cache, heads, at::kInt, "cnt: another size or device than the cache's").data_ptr();
     }
     void* p = cache.data_ptr();

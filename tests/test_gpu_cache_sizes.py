@@ -31,3 +31,15 @@ def test_calls_on_ordinary_caches_refuse_short_ones(dtype, torch_dtype):
     lte.lte_attn_decode(s, c, torch.cat([cache, cache[:16]]), one(), one(), one())     # a longer one holds the shape's
     torch.cuda.synchronize()
     assert lte.lte_device_status() == 0
+
+
+def test_no_list_is_needed_for_a_budget_of_none():
+    """R = 0: lte_cache_init_accum takes no idx, as lte_cache_init does and lte.h says."""
+    s = lte.shape(1, 2, 40, 64, 16, 0, lte.BF16)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((1, 2, 40, 64), generator=g, device="cuda").to(torch.bfloat16) for _ in "kv")
+    a, cnt = torch.rand((1, 2, 40), generator=g, device="cuda"), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    with_list = lte.lte_cache_init_accum(s, k, v, a, torch.empty((1, 2, 0), dtype=torch.int32, device="cuda"), cnt)
+    assert torch.equal(lte.lte_cache_init_accum(s, k, v, a, None, cnt), with_list)
+    with pytest.raises(TypeError):
+        lte.lte_cache_init_accum(lte.shape(1, 2, 40, 64, 16, 4, lte.BF16), k, v, a, None, cnt)
